@@ -1,0 +1,561 @@
+"""The operators of the 8-bit paged cache as their users call them, for timing.
+
+The cache (`tppsd.Cache`) holds keys and values of event sequences in pages of
+64 positions: e4m3 codes with a power-of-two scale per page, layer, head and
+side (keys, values), and the rows of the block that is still being filled as
+they came (the tail, a ring of 128 positions). Position i sees every block
+before its own in its 8-bit form and its own block as it came.
+
+Kinds of work:
+  attend  rows of new positions are appended to every layer's cache and attend
+          to it: a decoding step, a verify pass, a chunk of a history
+  append  rows are appended only, and what the cache holds of them read back
+  fork    sequences are continued by others: pages shared, open blocks copied,
+          what the others held freed
+  copy    sequences (and pages that they share) go to another cache's lowest
+          free pages
+
+With `own` false, `run` computes the same in elementary torch operations.
+"""
+import math
+
+import torch
+
+own = False
+
+BLOCK = 64           # positions of a page
+RING = 128           # rows of the tail
+E_MIN = -100         # least exponent of a scale
+
+
+def _attend(name, prec, layers, batch, heads, kv_heads, dh, ctx, rows, ragged=False, sink=False):
+    return {"name": name, "op": "attend", "prec": prec, "layers": layers, "batch": batch, "heads": heads,
+            "kv_heads": kv_heads, "dh": dh, "ctx": ctx, "rows": rows, "ragged": ragged, "sink": sink}
+
+
+def _append(name, prec, layers, batch, kv_heads, dh, ctx, rows, ragged=False):
+    return {"name": name, "op": "append", "prec": prec, "layers": layers, "batch": batch, "heads": kv_heads,
+            "kv_heads": kv_heads, "dh": dh, "ctx": ctx, "rows": rows, "ragged": ragged}
+
+
+def _fork(name, prec, layers, seqs, parents, kv_heads, dh, ctx):
+    return {"name": name, "op": "fork", "prec": prec, "layers": layers, "batch": seqs, "parents": parents,
+            "heads": kv_heads, "kv_heads": kv_heads, "dh": dh, "ctx": ctx, "ragged": True}
+
+
+def _copy(name, prec, layers, seqs, kv_heads, dh, ctx):
+    return {"name": name, "op": "copy", "prec": prec, "layers": layers, "batch": seqs, "heads": kv_heads,
+            "kv_heads": kv_heads, "dh": dh, "ctx": ctx, "ragged": True}
+
+
+def listed():
+    return [
+        # one user's short univariate sequence, verified with four drafts: launches and latency
+        _attend("attend_single", "fp32", 2, 1, 2, 2, 16, 220, 5),
+        # a study of 64 univariate sequences in fp32, ten drafts
+        _attend("attend_univariate", "fp32", 4, 64, 4, 4, 16, 550, 11),
+        # marked sequences with long histories, sixteen drafts: the cache streams from memory
+        _attend("attend_long", "bf16", 4, 32, 8, 8, 64, 4600, 17),
+        # single-token decoding of a ragged batch with shared heads, from a few tokens to long contexts
+        _attend("attend_grouped", "bf16", 1, 48, 32, 8, 128, 32000, 1, ragged=True),
+        # a chunk of histories of odd length after what was encoded before, with the extra key of score 0
+        _attend("attend_chunk", "bf16", 1, 16, 8, 8, 64, 2000, 1001, ragged=True, sink=True),
+        # a few rows of a few sequences, appended without queries
+        _append("append_rows", "bf16", 2, 5, 8, 32, 100, 11),
+        # whole histories encoded at once
+        _append("append_histories", "bf16", 4, 32, 8, 64, 0, 2560),
+        # one history continued seven times
+        _fork("fork_few", "fp32", 2, 8, 1, 4, 16, 230),
+        # resampling of many particles: an eighth of them continue
+        _fork("fork_particles", "bf16", 6, 2048, 256, 4, 32, 288),
+        # a few short sequences move to another cache
+        _copy("copy_few", "fp32", 2, 6, 2, 32, 200),
+        # what is left of a long-context batch moves to a smaller cache
+        _copy("copy_long", "bf16", 8, 64, 8, 64, 20000),
+    ]
+
+
+def _log(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(("attend", "attend", "attend", "append", "fork", "copy"))
+    prec = rng.choice(("bf16", "bf16", "fp32"))
+    dh = rng.choice((16, 32, 64, 128))
+    kv = rng.choice((1, 2, 4, 8))
+    layers = rng.choice((1, 2, 3, 4))
+    size = 2 if prec == "bf16" else 4
+    if op == "attend":
+        group = rng.choice((1, 1, 1, 2, 4, 8))
+        rows = rng.choice((1, _log(rng, 2, 33), _log(rng, 2, 33), _log(rng, 34, 1000)))
+        # keys of all layers and sequences within those of the largest listed case, and scores too
+        keys = min(500e6 / (2 * kv * dh * layers), 12e9 / (rows * kv * group * dh * layers))
+        if prec == "fp32":
+            keys /= 8
+        ctx = _log(rng, 1, int(min(32000, max(2, keys))))
+        batch = _log(rng, 1, int(min(512, max(1, keys / (ctx + rows)))))
+        c = _attend("", prec, layers, batch, kv * group, kv, dh, ctx, rows, rng.random() < 0.5, rng.random() < 0.3)
+    elif op == "append":
+        rows = _log(rng, 1, 2560)
+        ctx = rng.choice((0, _log(rng, 1, 500)))
+        most = 600e6 / (2 * size * kv * dh * layers * (rows + 64))
+        c = _append("", prec, layers, _log(rng, 1, int(min(256, max(1, most)))), kv, dh, ctx, rows, rng.random() < 0.5)
+    elif op == "fork":
+        seqs = _log(rng, 2, int(min(2048, max(2, 1.2e9 / (layers * kv * 2 * RING * dh * size)))))
+        most = 500e6 / (2 * kv * dh * layers * seqs)
+        c = _fork("", prec, layers, seqs, _log(rng, 1, max(1, seqs // 2)), kv, dh, _log(rng, 1, int(min(4000, max(2, most)))))
+    else:
+        seqs = _log(rng, 2, 64)
+        c = _copy("", prec, layers, seqs, kv, dh, _log(rng, 1, int(min(8000, max(2, 800e6 / (2 * kv * dh * layers * seqs))))))
+    del c["name"]
+    return c
+
+
+# ---- inputs ---------------------------------------------------------------
+
+def _lens(case):
+    """Positions that each sequence holds before the call: `ctx` less up to a
+    page, or, for ragged batches, spread over [1, ctx] by their logarithm."""
+    B, ctx = case["batch"], case["ctx"]
+    if ctx == 0:
+        return [0] * B
+    if not case["ragged"]:
+        return [max(1, ctx - (37 * i) % BLOCK) for i in range(B)]
+    return [max(1, min(ctx, int(round(ctx ** (((i * 7919) % B + 1) / B))))) for i in range(B)]
+
+
+def _counts(case):
+    """New positions of each sequence: all `rows`, or for ragged chunks as many and fewer."""
+    B, P = case["batch"], case["rows"]
+    return [max(1, P - (i * P) // (2 * B)) if case["ragged"] and P > 1 else P for i in range(B)]
+
+
+def _dtype(case):
+    return torch.bfloat16 if case["prec"] == "bf16" else torch.float32
+
+
+def _ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def _rows(gen, shape, dtype, keys):
+    """Key or value rows [.., heads, dh]: normal, every eighth channel of the keys four times as large."""
+    x = torch.randn(shape, generator=gen, device="cuda", dtype=torch.float32)
+    if keys:
+        x[..., ::8] *= 4.0
+    return x.to(dtype)
+
+
+def _inputs(case, seed):
+    """(generator, histories [(k, v) per layer: [B, longest, KV, dh]], new rows q, k, v [L, B, P, heads, dh])."""
+    gen = torch.Generator(device="cuda").manual_seed(int(seed))
+    L, B, KV, dh, dt = case["layers"], case["batch"], case["kv_heads"], case["dh"], _dtype(case)
+    n = max(_lens(case))
+    hist = [(_rows(gen, (B, n, KV, dh), dt, True), _rows(gen, (B, n, KV, dh), dt, False)) for _ in range(L)]
+    if case["op"] == "fork":
+        return gen, hist, None, None, None
+    P = case["rows"]
+    q = torch.randn((L, B, P, case["heads"], dh), generator=gen, device="cuda", dtype=torch.float32).to(dt)
+    k = _rows(gen, (L, B, P, KV, dh), dt, True)
+    v = _rows(gen, (L, B, P, KV, dh), dt, False)
+    return gen, hist, q, k, v
+
+
+def _pages_of(lens):
+    """Table of a cache that has encoded sequences of these lengths at once: the
+    pages of the first, then of the second, ... (-1: none)."""
+    held = [n // BLOCK for n in lens]
+    most = max(held + [1])
+    table = torch.full((len(lens), most), -1, dtype=torch.int64)
+    at = 0
+    for i, h in enumerate(held):
+        table[i, :h] = torch.arange(at, at + h)
+        at += h
+    return table.cuda(), at
+
+
+def prepare(case, seed):
+    if case["op"] == "copy":
+        return _prepare_copy(case, seed)
+    gen, hist, q, k, v = _inputs(case, seed)
+    lens, P = _lens(case), case.get("rows", 0)
+    B, L, KV, dh, dt = case["batch"], case["layers"], case["kv_heads"], case["dh"], _dtype(case)
+    s = {"case": case, "q": q, "k": k, "v": v}
+    if case["op"] != "fork":
+        s["counts"] = _ints(_counts(case))
+    if case["op"] == "attend":
+        s["o"] = torch.zeros((L, B, P, case["heads"], dh), dtype=dt, device="cuda")
+    if case["op"] == "append":
+        s["first"] = _ints([n // BLOCK * BLOCK for n in lens])
+        s["back"] = torch.zeros((2, L, B, P + BLOCK, KV, dh), dtype=dt, device="cuda")
+    if case["op"] == "fork":
+        par = case["parents"]
+        s["src"] = _ints([i % par for i in range(B - par)])
+        s["dst"] = _ints(list(range(par, B)))
+    if own:
+        from paper_2507_09252_amd import tppsd as tp
+        c = tp.Cache(L, case["heads"], KV, dh, case["prec"], B, max(lens) + P + BLOCK)
+        if max(lens) > 0:
+            c.tppsd_cache_begin(max(lens), counts=_ints(lens))
+            for layer, (hk, hv) in enumerate(hist):
+                c.tppsd_cache_append(layer, hk, hv)
+            c.tppsd_cache_commit()
+        s["cache"] = c
+        return s
+    table, used = _pages_of(lens)
+    n = _ints(lens).long()
+    tails = torch.zeros((L, B, KV, 2, RING, dh), dtype=dt, device="cuda")
+    if max(lens) > 0:
+        _to_tails(tails, torch.stack([h[0] for h in hist]), torch.stack([h[1] for h in hist]), n * 0, n)
+    s.update(table=table, lens=n, tails=tails)
+    if case["op"] == "fork":
+        s["refs"] = torch.zeros(max(used, 1), dtype=torch.int32, device="cuda")
+        s["refs"][:used] = 1
+        return s
+    s.update(pages=[], scales=[])
+    for side in range(2):
+        pool = torch.zeros((L, max(used, 1), KV, BLOCK, dh), dtype=torch.uint8, device="cuda")
+        scale = torch.ones((L, max(used, 1), KV), dtype=torch.float32, device="cuda")
+        for layer in range(L):
+            x = hist[layer][side]
+            nb = x.shape[1] // BLOCK
+            if nb == 0:
+                continue
+            codes, sc = _seal(x[:, :nb * BLOCK].reshape(B, nb, BLOCK, KV, dh).permute(0, 1, 3, 2, 4).float())
+            held = table[:, :nb] >= 0
+            pool[layer, table[:, :nb][held]] = codes.view(torch.uint8)[held]
+            scale[layer, table[:, :nb][held]] = sc[held]
+        s["pages"].append(pool)
+        s["scales"].append(scale)
+    return s
+
+
+def _copy_plan(case):
+    """(lengths of the source's sequences, sequences that move, free pages to spare)"""
+    lens = _lens(case)
+    return lens, list(range(0, case["batch"], 2)), 3
+
+
+def _prepare_copy(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(int(seed))
+    lens, moved, spare = _copy_plan(case)
+    L, KV, dh, dt, S = case["layers"], case["kv_heads"], case["dh"], _dtype(case), case["batch"]
+    table, used = _pages_of(lens)
+    n = max(used, 1)
+    # every fourth sequence is a fork of the first one: it shares that one's whole pages
+    shared = [i for i in range(4, S, 4)]
+    lens_now, held_now = list(lens), [x // BLOCK for x in lens]
+    for i in shared:
+        lens_now[i], held_now[i] = lens[0], lens[0] // BLOCK
+    live = held_now[0] + sum(held_now[i] for i in moved if i and i not in shared)
+    codes = torch.randint(-2 ** 31, 2 ** 31 - 1, (L, n, KV, 2 * BLOCK * dh // 4), generator=gen, device="cuda",
+                          dtype=torch.int32)
+    scales = torch.exp2(torch.randint(-9, 3, (L, n, KV, 2), generator=gen, device="cuda").float())
+    tails = torch.randn((L, S, KV, 2, RING, dh), generator=gen, device="cuda", dtype=torch.float32).to(dt)
+    s = {"case": case, "src": _ints(moved), "dst": _ints(list(range(len(moved))))}
+    if own:
+        from paper_2507_09252_amd import tppsd as tp
+        a = tp.Cache(L, KV, KV, dh, case["prec"], S, max(max(lens), 1), n)
+        b = tp.Cache(L, KV, KV, dh, case["prec"], len(moved), max(max(lens), 1), live + spare)
+        a.tppsd_cache_begin(max(lens), counts=_ints(lens))
+        a.tppsd_cache_commit()
+        if shared:
+            a.tppsd_cache_fork(_ints([0] * len(shared)), _ints(shared))
+        a.pages.view(torch.int32).copy_(codes)
+        a.scales.copy_(scales)
+        a.tails.copy_(tails)
+        s.update(cache=a, to=b)
+        return s
+    for i in shared:
+        table[i] = table[0]
+    width = (max(max(lens), 1) + BLOCK - 1) // BLOCK
+    table = torch.nn.functional.pad(table, (0, width))[:, :width]
+    held = torch.arange(width, device="cuda")[None, :] < torch.tensor(held_now, device="cuda")[:, None]
+    s.update(table=torch.where(held, table, -1), lens=_ints(lens_now), codes=codes, scales=scales, tails=tails,
+             to={"codes": torch.zeros((L, live + spare, KV, 2 * BLOCK * dh // 4), dtype=torch.int32, device="cuda"),
+                 "scales": torch.zeros((L, live + spare, KV, 2), device="cuda"),
+                 "tails": torch.zeros((L, len(moved), KV, 2, RING, dh), dtype=dt, device="cuda")})
+    return s
+
+
+# ---- the plain forms ------------------------------------------------------
+
+def _pow2(e):
+    return ((e.to(torch.int32) + 127) << 23).view(torch.float32)
+
+
+def _seal(x):
+    """e4m3 codes and scales of blocks x [.., BLOCK, dh] (fp32): the scale is the
+    least power of two 2^e with max |x| <= 448 2^e."""
+    top = torch.where(torch.isfinite(x), x.abs(), 0.0).amax((-2, -1))
+    m, e = torch.frexp(top)
+    e = torch.where(m <= 0.875, e - 9, e - 8).clamp(min=E_MIN)
+    e = torch.where(top > 0, e, 0)
+    return (x * _pow2(-e)[..., None, None]).to(torch.float8_e4m3fn), _pow2(e)
+
+
+def _to_tails(tails, k, v, start, count):
+    """Rows k, v [L, B, P, KV, dh] at positions start .. start + count - 1 into
+    the ring [L, B, KV, 2, RING, dh]: those of the last two blocks."""
+    slot = torch.arange(RING, device="cuda")[None, :]
+    end = (start + count)[:, None]
+    pos = end - 1 - (end - 1 - slot) % RING                      # last position below end in this slot
+    low = torch.maximum(start[:, None], ((end - 1) // BLOCK - 1) * BLOCK)
+    ok = (pos >= low) & (pos >= 0)
+    row = (pos - start[:, None]).clamp(0, k.shape[2] - 1)
+    at = row[None, :, :, None, None].expand(k.shape[0], -1, -1, k.shape[3], k.shape[4])
+    new = torch.stack([torch.gather(x, 2, at).permute(0, 1, 3, 2, 4) for x in (k, v)], 3)
+    tails.copy_(torch.where(ok[None, :, None, None, :, None], new, tails))
+
+
+def _window(s, side):
+    """Rows of the blocks that the new positions touch, as they came (fp32):
+    [L, B, W, KV, dh] from position `base` on, zero outside the sequence."""
+    x, tails, n, count = s["v" if side else "k"], s["tails"], s["lens"], s["counts"].long()
+    W = (x.shape[2] + 2 * BLOCK - 2) // BLOCK * BLOCK
+    base = n // BLOCK * BLOCK
+    pos = base[:, None] + torch.arange(W, device="cuda")[None, :]
+    old = pos < n[:, None]
+    new = ~old & (pos < (n + count)[:, None])
+    at = (pos % RING)[None, :, None, :, None].expand(x.shape[0], -1, x.shape[3], -1, x.shape[4])
+    kept = torch.gather(tails[:, :, :, side], 3, at).permute(0, 1, 3, 2, 4)
+    at = (pos - n[:, None]).clamp(0, x.shape[2] - 1)[None, :, :, None, None].expand(x.shape[0], -1, -1, x.shape[3], x.shape[4])
+    come = torch.gather(x, 2, at)
+    rows = torch.where(old[None, :, :, None, None], kept, torch.where(new[None, :, :, None, None], come, 0.0))
+    return rows.float(), pos, base
+
+
+def _held(rows):
+    """A window's rows in their 8-bit form (fp32)."""
+    L, B, W, KV, dh = rows.shape
+    codes, sc = _seal(rows.reshape(L, B, W // BLOCK, BLOCK, KV, dh).transpose(3, 4))
+    return (codes.float() * sc[..., None, None]).transpose(3, 4).reshape(L, B, W, KV, dh)
+
+
+def _plain_attend(s):
+    case, q = s["case"], s["q"]
+    L, B, P, H, dh = q.shape
+    KV, G, dt = case["kv_heads"], H // case["kv_heads"], _dtype(case)
+    n, count = s["lens"], s["counts"].long()
+    kx, pos, base = _window(s, 0)
+    vx = _window(s, 1)[0]
+    pages = s["table"].shape[1]
+    keys, values = [], []
+    for side, to, exact in ((0, keys, kx), (1, values, vx)):
+        pool = s["pages"][side][:, s["table"].clamp(min=0)].view(torch.float8_e4m3fn).float()
+        pool *= s["scales"][side][:, s["table"].clamp(min=0)][..., None, None]
+        to.append(pool.transpose(3, 4).reshape(L, B, pages * BLOCK, KV, dh))
+        to.append(_held(exact))
+        to.append(exact)
+    keys, values = torch.cat(keys, 2).permute(0, 1, 3, 4, 2), torch.cat(values, 2).permute(0, 1, 3, 2, 4)
+    at = n[:, None] + torch.arange(P, device="cuda")[None, :]
+    j = torch.arange(pages * BLOCK, device="cuda")
+    before = (j[None, None, :] < base[:, None, None]).expand(B, P, -1)
+    sealed = pos[:, None, :] // BLOCK < at[:, :, None] // BLOCK
+    same = (pos[:, None, :] // BLOCK == at[:, :, None] // BLOCK) & (pos[:, None, :] <= at[:, :, None])
+    seen = torch.cat([before, sealed, same], 2)
+    qr = q.float().reshape(L, B, P, KV, G, dh).permute(0, 1, 3, 4, 2, 5).reshape(L, B, KV, G * P, dh)
+    sc = torch.matmul(qr, keys).reshape(L, B, KV, G, P, -1).mul_(1.0 / math.sqrt(dh))
+    sc.masked_fill_(~seen[None, :, None, None], -math.inf)
+    m = sc.amax(-1, keepdim=True)
+    if case["sink"]:
+        m = m.clamp(min=0.0)
+    sc = sc.sub_(m).exp_()
+    total = sc.sum(-1, keepdim=True)
+    if case["sink"]:
+        total = total + torch.exp(-m)
+    o = torch.matmul(sc.reshape(L, B, KV, G * P, -1), values).reshape(L, B, KV, G, P, dh) / total
+    o = o.permute(0, 1, 4, 2, 3, 5).reshape(L, B, P, H, dh)
+    ok = torch.arange(P, device="cuda")[None, :] < count[:, None]
+    o = torch.where(ok[None, :, :, None, None], o.to(dt), s["o"])
+    _to_tails(s["tails"], s["k"], s["v"], n, count)
+    return {"o": o, "tails": s["tails"]}
+
+
+def _plain_append(s):
+    dt = _dtype(s["case"])
+    n, end = s["lens"], s["lens"] + s["counts"].long()
+    back, R = [], s["back"].shape[3]
+    for side in (0, 1):
+        rows, pos, base = _window(s, side)
+        sealed = (pos // BLOCK + 1) * BLOCK <= end[:, None]
+        held = torch.where(sealed[None, :, :, None, None], _held(rows), rows).to(dt)
+        held = torch.nn.functional.pad(held, (0, 0, 0, 0, 0, max(0, R - held.shape[2])))[:, :, :R]
+        inside = base[:, None] + torch.arange(R, device="cuda")[None, :] < end[:, None]
+        back.append(torch.where(inside[None, :, :, None, None], held, s["back"][side]))
+    _to_tails(s["tails"], s["k"], s["v"], n, s["counts"].long())
+    return {"k": back[0], "v": back[1], "tails": s["tails"]}
+
+
+def _plain_fork(s):
+    src, dst, n = s["src"].long(), s["dst"].long(), s["lens"]
+    table, refs = s["table"], s["refs"]
+    for rows, by in ((dst, -1), (src, 1)):   # what the destinations held is let go, what they share is held
+        p = table[rows].reshape(-1)
+        refs.index_add_(0, p.clamp(min=0), torch.where(p >= 0, by, 0).to(torch.int32))
+    table[dst], n[dst] = table[src], n[src]
+    base = n[src] // BLOCK * BLOCK
+    slot = torch.arange(RING, device="cuda")[None, :]
+    pos = base[:, None] + (slot - base[:, None]) % RING
+    ok = (pos < n[src][:, None])[None, :, None, None, :, None]
+    s["tails"][:, dst] = torch.where(ok, s["tails"][:, src], s["tails"][:, dst])
+    return {"table": table.to(torch.int32), "lens": n.to(torch.int32), "refs": refs, "tails": s["tails"]}
+
+
+def _plain_copy(s):
+    src, to, n = s["src"].long(), s["to"], s["lens"].long()
+    table = s["table"][src]
+    pages, room = s["codes"].shape[1], to["codes"].shape[1]
+    used = torch.zeros(pages + 1, dtype=torch.int64, device="cuda")
+    used[torch.where(table >= 0, table, pages).reshape(-1)] = 1
+    rank = torch.cumsum(used[:pages], 0) - 1                     # the lowest free pages, in the source's order
+    come = torch.full((room + 1,), -1, dtype=torch.int64, device="cuda")
+    come[torch.where(used[:pages] > 0, rank, room)] = torch.arange(pages, device="cuda")
+    come = come[:room]
+    for key in ("codes", "scales"):
+        kept = (come >= 0).reshape((1, -1) + (1,) * (s[key].dim() - 2))
+        to[key].copy_(torch.where(kept, s[key][:, come.clamp(min=0)], to[key]))
+    table = torch.where(table >= 0, rank[table.clamp(min=0)], -1)
+    n = n[src]
+    base = n // BLOCK * BLOCK
+    slot = torch.arange(RING, device="cuda")[None, :]
+    ok = (base[:, None] + (slot - base[:, None]) % RING < n[:, None])[None, :, None, None, :, None]
+    to["tails"].copy_(torch.where(ok, s["tails"][:, src], to["tails"]))
+    return {"codes": to["codes"], "scales": to["scales"], "tails": to["tails"], "table": table.to(torch.int32),
+            "lens": n.to(torch.int32)}
+
+
+# ---- the framework's calls ------------------------------------------------
+
+def _own_attend(s):
+    c, case = s["cache"], s["case"]
+    c.tppsd_cache_begin(case["rows"], counts=s["counts"])
+    for layer in range(case["layers"]):
+        c.tppsd_cache_attend(layer, s["q"][layer], s["k"][layer], s["v"][layer], out=s["o"][layer], sink=case["sink"])
+    return {"o": s["o"], "tails": c.tails}
+
+
+def _own_append(s):
+    c, case, (k, v) = s["cache"], s["case"], s["back"]
+    c.tppsd_cache_begin(case["rows"], counts=s["counts"])
+    for layer in range(case["layers"]):
+        c.tppsd_cache_append(layer, s["k"][layer], s["v"][layer])
+        c.tppsd_cache_read(layer, s["first"], case["rows"] + BLOCK, k[layer], v[layer])
+    return {"k": k, "v": v, "tails": c.tails}
+
+
+def _own_fork(s):
+    c = s["cache"]
+    c.tppsd_cache_fork(s["src"], s["dst"])
+    pages = (max(_lens(s["case"])) // BLOCK) or 1
+    used = sum(n // BLOCK for n in _lens(s["case"])) or 1
+    return {"table": c.table[:, :pages], "lens": c.lens, "refs": c.refs[:used], "tails": c.tails}
+
+
+def _own_copy(s):
+    c = s["to"]
+    c.tppsd_cache_copy(s["cache"], s["src"], s["dst"])
+    return {"codes": c.pages.view(torch.int32), "scales": c.scales, "tails": c.tails, "table": c.table, "lens": c.lens}
+
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return {"attend": _own_attend, "append": _own_append, "fork": _own_fork, "copy": _own_copy}[op](state)
+    return {"attend": _plain_attend, "append": _plain_append, "fork": _plain_fork, "copy": _plain_copy}[op](state)
+
+
+# ---- what a pass cannot do without ----------------------------------------
+
+def work(case):
+    L, KV, dh = case["layers"], case["kv_heads"], case["dh"]
+    e = 2 if case["prec"] == "bf16" else 4
+    lens = _lens(case)
+    row = 2 * KV * dh * L                                        # keys and values of a position, elements
+    if case["op"] == "attend":
+        P, H, nbytes, flops = _counts(case), case["heads"], 0, 0
+        for n, p in zip(lens, P):
+            sealed, tail = n // BLOCK * BLOCK, n % BLOCK
+            nbytes += row * (sealed + tail * e) + sealed // BLOCK * 2 * KV * L * 4
+            nbytes += p * row * e + min(p, RING) * row * e + L * 2 * p * H * dh * e
+            nbytes += ((n + p) // BLOCK - n // BLOCK) * BLOCK * row
+            flops += 4 * L * H * dh * (p * n + p * (p + 1) // 2)
+        return {"bytes": nbytes, "flops": flops}
+    if case["op"] == "append":
+        nbytes = 0
+        for n, p in zip(lens, _counts(case)):
+            sealed = ((n + p) // BLOCK - n // BLOCK) * BLOCK
+            nbytes += p * row * e + n % BLOCK * row * e + min(p, RING) * row * e + sealed * row   # append
+            nbytes += sealed * row + (n % BLOCK + p) * row * e + (n % BLOCK + p - sealed) * row * e   # read back
+        return {"bytes": nbytes, "flops": 0}
+    if case["op"] == "fork":
+        par, nbytes = case["parents"], 0
+        for i in range(len(lens) - par):
+            n = lens[i % par]
+            nbytes += 2 * (n % BLOCK) * row * e + 3 * 4 * (n // BLOCK + lens[par + i] // BLOCK)
+        return {"bytes": nbytes, "flops": 0}
+    lens, moved, _ = _copy_plan(case)
+    shared = set(range(4, case["batch"], 4))
+    nbytes = 0
+    for i in moved:
+        n = lens[0] if i in shared else lens[i]
+        nbytes += 2 * (n % BLOCK) * row * e + 8 * (n // BLOCK)
+        if i not in shared:
+            nbytes += 2 * n // BLOCK * (row * BLOCK + 2 * KV * L * 4)
+    return {"bytes": nbytes, "flops": 0}
+
+
+# ---- the definition in 64 bits --------------------------------------------
+
+def _e4m3(x):
+    """What blocks x [n, BLOCK, KV, dh] (float64) are held as: e4m3 values times a power of two."""
+    def two(e):
+        return ((e.long() + 1023) << 52).view(torch.float64)
+    top = x.abs().amax((1, 3), keepdim=True)
+    m, e = torch.frexp(top)                                      # top / 448 = (m / 0.875) 2^(e - 9)
+    e = torch.where(top > 0, torch.where(m > 0.875, e - 8, e - 9).clamp(min=E_MIN), 0)
+    y = x * two(-e)
+    step = two((torch.frexp(y)[1] - 1).clamp(min=-6) - 3)        # three bits below the leading one
+    return torch.round(y / step) * step * two(e)
+
+
+def exact(case, seed):
+    if case["op"] not in ("attend", "append"):
+        return None                                              # bytes and whole numbers that move
+    lens, counts = _lens(case), _counts(case)
+    if case["op"] == "attend" and case["batch"] * case["layers"] > 600:
+        return None
+    _, hist, q, k, v = _inputs(case, seed)
+    L, KV, dh, P = case["layers"], case["kv_heads"], case["dh"], case["rows"]
+    G = case["heads"] // KV
+    out = torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    back = torch.zeros((2, L, case["batch"], P + BLOCK, KV, dh), dtype=torch.float64, device="cuda")
+    for layer in range(L):
+        for b, (n, p) in enumerate(zip(lens, counts)):
+            came = [torch.cat([hist[layer][side][b, :n], x[layer, b, :p]]).double() for side, x in ((0, k), (1, v))]
+            whole = (n + p) // BLOCK * BLOCK
+            held = [torch.cat([_e4m3(x[:whole].reshape(-1, BLOCK, KV, dh)).reshape(whole, KV, dh), x[whole:]])
+                    for x in came]
+            if case["op"] == "append":
+                for side in range(2):
+                    back[side, layer, b, :n % BLOCK + p] = held[side][n // BLOCK * BLOCK:]
+                continue
+            qb = q[layer, b, :p].double().reshape(p, KV, G, dh).permute(1, 2, 0, 3).reshape(KV, G * p, dh)
+            # the queries of each block see the blocks before as they are held, their own as it came
+            for a in range(n // BLOCK * BLOCK, n + p, BLOCK):
+                i0, i1 = max(a, n), min(a + BLOCK, n + p)
+                kk = torch.cat([held[0][:a], came[0][a:i1]]).permute(1, 2, 0)
+                vv = torch.cat([held[1][:a], came[1][a:i1]]).permute(1, 0, 2)
+                qq = qb.reshape(KV, G, p, dh)[:, :, i0 - n:i1 - n].reshape(KV, -1, dh)
+                sc = torch.matmul(qq, kk).reshape(KV, G, i1 - i0, i1) / math.sqrt(dh)
+                late = torch.arange(i1, device="cuda")[None, :] > torch.arange(i0, i1, device="cuda")[:, None]
+                sc = sc.masked_fill(late, -math.inf)
+                if case["sink"]:
+                    sc = torch.nn.functional.pad(sc, (1, 0))
+                w = torch.softmax(sc, -1)[..., 1 if case["sink"] else 0:]
+                o = torch.matmul(w.reshape(KV, G * (i1 - i0), i1), vv).reshape(KV, G, i1 - i0, dh)
+                out[layer, b, i0 - n:i1 - n] = o.permute(2, 0, 1, 3).reshape(i1 - i0, G * KV, dh)
+    if case["op"] == "attend":
+        return {"o": out, "tails": None}
+    return {"k": back[0], "v": back[1], "tails": None}
