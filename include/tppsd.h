@@ -67,6 +67,10 @@ extern "C" {
 #define TPPSD_STATUS_CAPACITY  1u  /* an append would pass max_events           */
 #define TPPSD_STATUS_NONFINITE 2u  /* a log-density or sampled interval was NaN/Inf */
 #define TPPSD_STATUS_AR_CAP    4u  /* Theorem-1 loop hit TPPSD_AR_ITER_CAP        */
+#define TPPSD_STATUS_PAGES     8u  /* cache: no free page for a row; it was left out */
+#define TPPSD_STATUS_SEQUENCE 16u  /* cache: a sequence that does not exist, or named twice */
+#define TPPSD_STATUS_OPEN     32u  /* cache: a length inside a block whose rows are no longer held;
+                                      rounded down to the block */
 
 #define TPPSD_AR_ITER_CAP (1 << 20)
 
@@ -355,6 +359,140 @@ typedef struct tppsd_timing {
 } tppsd_timing;
 int tppsd_timing_enable(tppsd_state *s, int modes);
 int tppsd_timing_read(tppsd_state *s, tppsd_timing *out);
+
+/* ---- 8-bit paged cache ---------------------------------------------------------
+ * Keys and values of many sequences in pages of TPPSD_CACHE_BLOCK positions,
+ * as e4m3 codes with one power-of-two scale for each page, layer, key/value
+ * head and side (keys, values): half the bytes of bf16. Codes are
+ * rne(x 2^-e), e the least integer >= -100 with max |x| <= 448 2^e over the
+ * page's finite elements; elements that are not finite become NaN. A block
+ * that is not full yet is kept as its rows came (in the cache's precision), so
+ * an element is rounded once, under the maximum of its whole block.
+ *
+ * Position i attends to the blocks before its own in their 8-bit form and to
+ * its own block, up to itself, as the rows came. That depends on i alone, not
+ * on how the calls cut a sequence: single steps, verify passes and prefill
+ * chunks compute the same function.
+ *
+ * A call sequence: tppsd_cache_begin (which sequences, how many positions),
+ * then per layer tppsd_cache_attend or tppsd_cache_append, then
+ * tppsd_cache_commit (how many of the positions stay). All of them work from
+ * counters on the device, so a captured sequence can be replayed. Page ids are
+ * given out lowest first, in the batch's order. One stream at a time uses a
+ * cache; calls are enqueued and asynchronous, sticky status bits report what
+ * the device finds (tppsd_cache_status). */
+#define TPPSD_CACHE_BLOCK 64    /* positions of a page */
+#define TPPSD_CACHE_RING 128    /* positions that a sequence's tail has rows for */
+
+/* n_heads query heads share n_kv_heads key/value heads (a divisor): query head
+ * h reads head h / (n_heads / n_kv_heads). d_head 16, 32, 64 or 128; prec: type
+ * of q, k, v, o and the tails. n_pages 0: max_seqs ceil(max_events / 64), enough
+ * for every sequence at its longest; fewer where sequences share pages. */
+typedef struct {
+  int32_t n_layers, n_heads, n_kv_heads, d_head, prec;
+  int32_t max_seqs, max_events, n_pages;
+} tppsd_cache_cfg;
+
+typedef struct tppsd_cache tppsd_cache;   /* opaque host handle */
+
+/* Rows of a call, [B, n_new] of them, elements of the cache's precision: row
+ * (i, p) of k starts (i n_new + p) ldk elements on and holds n_kv_heads d_head
+ * (q, o: n_heads d_head). Pointers and row strides are multiples of 16 bytes.
+ * tppsd_cache_append reads k and v alone. */
+typedef struct {
+  const void *q, *k, *v;
+  void *o;
+  int64_t ldq, ldk, ldv, ldo;
+} tppsd_cache_rows;
+
+/* Device workspace of a cache. Errors: TPPSD_E_ARG, TPPSD_E_CONFIG. */
+int tppsd_cache_bytes(const tppsd_cache_cfg *cfg, size_t *bytes);
+
+/* Where an array of the cache lies in its workspace: "pages" [n_layers][n_pages]
+ * [n_kv_heads][2][64 d_head] uint8 (codes, in an order of the library's own),
+ * "scales" [n_layers][n_pages][n_kv_heads][2] float, "tails" [n_layers][max_seqs]
+ * [n_kv_heads][2][128][d_head] (row of position i: i mod 128), "table" [max_seqs]
+ * [ceil(max_events / 64)] int32 (-1: no page), "lens" [max_seqs] int32, "refs"
+ * [n_pages] int32. For reading; returns TPPSD_E_ARG past the last. */
+int tppsd_cache_entry(const tppsd_cache_cfg *cfg, int index, const char **name, size_t *offset);
+
+/* Creates a cache in the caller's workspace (256-byte aligned). Enqueues
+ * nothing: tppsd_cache_reset comes next. Errors: TPPSD_E_ARG, TPPSD_E_CONFIG,
+ * TPPSD_E_WORKSPACE. */
+int  tppsd_cache_create(const tppsd_cache_cfg *cfg, void *d_workspace, size_t ws_bytes, tppsd_cache **out);
+void tppsd_cache_destroy(tppsd_cache *c);
+
+/* Empties every sequence, frees every page and clears the status bits. */
+int tppsd_cache_reset(tppsd_cache *c, hipStream_t stream);
+
+/* Plans a call for B rows of n_new positions: row i brings d_counts[i] of them
+ * (clamped to 0..n_new; NULL: all) to sequence d_seqs[i] (NULL: i), behind its
+ * committed ones. Takes a page for every block that becomes whole. A row is
+ * left out (nothing appended, its output rows left as they were) when its
+ * sequence does not exist or an earlier row names it (TPPSD_STATUS_SEQUENCE),
+ * when it would pass max_events (TPPSD_STATUS_CAPACITY), or when the pages that
+ * it and the rows before it need are not there (TPPSD_STATUS_PAGES). A plan that
+ * was not committed is dropped. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no reset),
+ * TPPSD_E_HIP. */
+int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, const int32_t *d_counts,
+                      hipStream_t stream);
+
+/* Appends the planned rows of one layer. Every layer is appended once before
+ * tppsd_cache_commit. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no plan), TPPSD_E_HIP. */
+int tppsd_cache_append(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, hipStream_t stream);
+
+/* Appends the planned rows of one layer and attends: o = softmax(scale q K^T) V
+ * over what each position sees (above); sink != 0: one more key of score 0 and
+ * value 0 (the 1 + sum f of AttNHP). Scores, the softmax's maximum and sum and
+ * the output are accumulated in fp32. A position whose own visible keys or
+ * values are not finite gets NaN; positions that do not see them are not
+ * touched. o may be q's memory, not k's or v's. Errors: as tppsd_cache_append, scale not
+ * positive and finite: TPPSD_E_ARG. */
+int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, float scale, int sink,
+                       hipStream_t stream);
+
+/* Ends the call: row i keeps the first d_accept[i] of its positions (clamped to
+ * 0..its count; NULL: all). What is dropped may be brought again. After a call of
+ * more than 64 positions a length inside a block before the last two is rounded
+ * down to that block (TPPSD_STATUS_OPEN). Errors: TPPSD_E_ORDER, TPPSD_E_HIP. */
+int tppsd_cache_commit(tppsd_cache *c, const int32_t *d_accept, hipStream_t stream);
+
+/* Shortens sequences d_seqs[0 .. n) to d_lens (NULL: 0; a length at or past a
+ * sequence's own leaves it) and frees the pages past it that no other sequence
+ * holds. A length inside a block whose rows are no longer in the tail is
+ * rounded down to the block (TPPSD_STATUS_OPEN): lengths in the open block, and
+ * multiples of 64, always stand. A sequence named twice gets the shorter length.
+ * Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+int tppsd_cache_truncate(tppsd_cache *c, int n, const int32_t *d_seqs, const int32_t *d_lens, hipStream_t stream);
+
+/* d_dst[j] becomes a copy of sequence d_src[j], j < n <= max_seqs: what it held is freed,
+ * whole pages are shared (they are never written again) and the open block's
+ * rows copied. A source may be named many times; a pair whose destination
+ * another pair names before it or as a source is left out
+ * (TPPSD_STATUS_SEQUENCE). Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+int tppsd_cache_fork(tppsd_cache *c, int n, const int32_t *d_src, const int32_t *d_dst, hipStream_t stream);
+
+/* Sequences d_dst[j] of `to` become copies of sequences d_src[j] of `from`, in
+ * pages of `to`: its lowest free ones, in the order of the source's page ids,
+ * pages that several of the listed sequences share once. So a cache moves
+ * into a smaller or larger workspace, without gaps. A pair is left out as in
+ * tppsd_cache_fork (here a source may be any), or when its length passes to's
+ * max_events (TPPSD_STATUS_CAPACITY); when the free pages do not hold all pairs,
+ * every destination is left empty (TPPSD_STATUS_PAGES). Status bits are
+ * those of `to`. Both caches have the same layers, key/value heads, d_head and
+ * precision. Errors: TPPSD_E_ARG, TPPSD_E_CONFIG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+int tppsd_cache_copy(tppsd_cache *to, tppsd_cache *from, int n, const int32_t *d_src, const int32_t *d_dst,
+                     hipStream_t stream);
+
+/* Rows of positions d_first[i] (NULL: 0) .. + count - 1 of sequences d_seqs[i]
+ * (NULL: i) as the cache holds them, appended and not yet committed ones
+ * included, into d_k and d_v [n, count, n_kv_heads, d_head]; rows past a sequence's end are
+ * left as they were. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+int tppsd_cache_read(tppsd_cache *c, int layer, int n, const int32_t *d_seqs, const int32_t *d_first, int count,
+                     void *d_k, void *d_v, hipStream_t stream);
+
+/* Synchronises the stream and reads the status bits since the last reset. */
+int tppsd_cache_status(tppsd_cache *c, hipStream_t stream, uint32_t *bits);
 
 /* Thread-local description of the last error on this thread. */
 const char *tppsd_last_error(void);

@@ -19,6 +19,10 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libtppsd.so")
 ARCH = "gfx950"
 
+DEVICE_SRCS = ("tppsd_kernels.hip", "tppsd_attention.hip", "tppsd_poisson.hip", "tppsd_draft_rows.hip",
+               "tppsd_draft_regs.hip", "tppsd_cache.hip", "tppsd_cache_attn.hip")
+HOST_SRCS = ("tppsd.cpp", "tppsd_cache.cpp")
+
 HIPCC_FLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC",
     # no packed-fp32 instructions in device code
@@ -67,8 +71,7 @@ def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     inc = ["-I", os.path.join(ROOT, "include"), "-I", CSRC]
     from concurrent.futures import ThreadPoolExecutor
-    srcs = ("tppsd_kernels.hip", "tppsd_attention.hip", "tppsd_poisson.hip", "tppsd_draft_rows.hip",
-            "tppsd_draft_regs.hip", "tppsd.cpp")
+    srcs = DEVICE_SRCS + HOST_SRCS
     objs = [os.path.join(BUILD, src + ".o") for src in srcs]
     cmds = [[hipcc] + source_flags(src) + inc + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", obj]
             for src, obj in zip(srcs, objs)]
@@ -84,15 +87,13 @@ def build(verbose: bool = False) -> str:
 
 
 def build_host_sanitized(out_dir: str, verbose: bool = False) -> str:
-    """The library with its host source (tppsd.cpp) built under
+    """The library with its host sources (HOST_SRCS) built under
     AddressSanitizer and UndefinedBehaviorSanitizer and the device sources as
     in build(), whose objects it reuses (built first if missing), for CPU
     tests of the host-side paths. Load it with the sanitizer runtime
     preloaded (sanitizer_runtime())."""
     hipcc = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
-    dev = ("tppsd_kernels.hip", "tppsd_attention.hip", "tppsd_poisson.hip", "tppsd_draft_rows.hip",
-           "tppsd_draft_regs.hip")
-    objs = [os.path.join(BUILD, src + ".o") for src in dev]
+    objs = [os.path.join(BUILD, src + ".o") for src in DEVICE_SRCS]
     if not all(os.path.exists(o) for o in objs):
         build(verbose)
     os.makedirs(out_dir, exist_ok=True)
@@ -100,11 +101,13 @@ def build_host_sanitized(out_dir: str, verbose: bool = False) -> str:
     san = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
            "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-omit-frame-pointer"]
     flags = [f for f in HIPCC_FLAGS if f != "-O3"] + ["-O1", "-g"]
-    host_obj = os.path.join(out_dir, "tppsd_san.cpp.o")
-    _run([hipcc] + flags + san + inc + ["-x", "hip", "-c", os.path.join(CSRC, "tppsd.cpp"), "-o", host_obj], verbose)
+    host_objs = []
+    for src in HOST_SRCS:
+        host_objs.append(os.path.join(out_dir, src + ".san.o"))
+        _run([hipcc] + flags + san + inc + ["-x", "hip", "-c", os.path.join(CSRC, src), "-o", host_objs[-1]], verbose)
     tlib = _torch_lib_dir()
     out = os.path.join(out_dir, "libtppsd_san.so")
-    _run([_clangxx(), "-shared", "-fsanitize=address,undefined", "-shared-libasan", "-o", out] + objs + [host_obj] +
+    _run([_clangxx(), "-shared", "-fsanitize=address,undefined", "-shared-libasan", "-o", out] + objs + host_objs +
          [f"-L{tlib}", "-l:libamdhip64.so", f"-Wl,-rpath,{tlib}"], verbose)
     return out
 

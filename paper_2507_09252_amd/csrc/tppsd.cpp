@@ -25,7 +25,7 @@
 
 using namespace tppsd;
 
-namespace {
+namespace tppsd {
 
 thread_local std::string g_err;
 
@@ -44,6 +44,10 @@ int hip_check(const char *what) {
   if (e != hipSuccess) return fail(TPPSD_E_HIP, "%s: %s", what, hipGetErrorString(e));
   return TPPSD_OK;
 }
+
+}  // namespace tppsd
+
+namespace {
 
 int hip_check_rc(hipError_t e) {
   return e == hipSuccess ? TPPSD_OK : fail(TPPSD_E_HIP, "timing event: %s", hipGetErrorString(e));

@@ -1,0 +1,652 @@
+// 8-bit paged cache: page bookkeeping, appending (quantisation), reading back,
+// forks and copies. Page ids are given out lowest first and freed into a
+// bitmap, so that tables depend on the calls alone, never on the order in
+// which atomics arrive.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/tppsd.h"
+#include "tppsd_cache.h"
+#include "tppsd_device.h"
+
+namespace tppsd {
+
+namespace {
+
+constexpr int PLAN_NT = 1024;   // the bookkeeping scans run in one workgroup
+
+__device__ __forceinline__ int ld_agent(const int32_t *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t ld_agent(const uint32_t *p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void st_agent(int32_t *p, int v) {
+  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// exclusive sum of v over the workgroup's threads in order; *total: the whole sum
+__device__ int block_scan(int v, int *total) {
+  __shared__ int sums[PLAN_NT / 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();   // (the last call's sums have been read)
+  if (lane == 63) sums[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN_NT / 64; ++w) {
+    const int s = sums[w];
+    before += w < wave ? s : 0;
+    all += s;
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// The set bits of bits[0 .. nbits) in ascending order into list, until at least
+// `want` are found; returns how many (at most want).
+__device__ int list_bits(const uint32_t *bits, int nbits, int want, int32_t *list) {
+  const int words = (nbits + 31) / 32;
+  int found = 0;
+  for (int w0 = 0; w0 < words && found < want; w0 += PLAN_NT) {
+    const int w = w0 + threadIdx.x;
+    uint32_t m = w < words ? ld_agent(bits + w) : 0u;
+    int total;
+    int k = found + block_scan(__popc(m), &total);
+    while (m && k < want) {
+      const int bit = __ffs(m) - 1;
+      m &= m - 1;
+      list[k++] = w * 32 + bit;
+    }
+    found += total;
+  }
+  __syncthreads();   // the list is complete (one workgroup: its global writes are visible past the barrier)
+  return min(found, want);
+}
+
+// gives a page back: the last holder sets its bit
+__device__ __forceinline__ void page_drop(const CacheDev &c, int page) {
+  if (atomicSub(&c.refs[page], 1) == 1) atomicOr(&c.freeb[page >> 5], 1u << (page & 31));
+}
+
+__global__ void k_cache_reset(CacheDev c) {
+  const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
+  for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
+  for (size_t j = i; j < (size_t)c.S; j += n) c.lens[j] = c.held[j] = c.low[j] = c.pend[j] = 0;
+  for (size_t j = i; j < (size_t)c.n_pages; j += n) c.refs[j] = 0;
+  for (size_t j = i; j < (size_t)(c.n_pages + 31) / 32; j += n) {
+    const int left = c.n_pages - (int)j * 32;
+    c.freeb[j] = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
+    c.mark[j] = 0u;
+  }
+  if (i == 0) *c.status = 0u;
+}
+
+// Plans a call: which sequence each row of the batch names, its first new
+// position and how many it brings; pages for the blocks that become whole; and
+// the work items of the split attention. One workgroup: the whole batch's
+// bookkeeping is a few thousand integers.
+__global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
+  const int tid = threadIdx.x;
+  const int per = (b.B + PLAN_NT - 1) / PLAN_NT, i0 = min(b.B, tid * per), i1 = min(b.B, i0 + per);
+  if (b.seqs) {
+    // a sequence that is named twice belongs to the first row that names it
+    for (int i = i0; i < i1; ++i) {
+      const int s = b.seqs[i];
+      if (s >= 0 && s < c.S) st_agent(&c.owner[s], INT32_MAX);
+    }
+    __threadfence();
+    __syncthreads();
+    for (int i = i0; i < i1; ++i) {
+      const int s = b.seqs[i];
+      if (s >= 0 && s < c.S) atomicMin(&c.owner[s], i);
+    }
+    __threadfence();
+    __syncthreads();
+  }
+  int need_sum = 0;
+  for (int i = i0; i < i1; ++i) {
+    int s = b.seqs ? b.seqs[i] : i;
+    bool ok = s >= 0 && s < c.S;
+    if (ok && b.seqs) ok = ld_agent(&c.owner[s]) == i;
+    if (!ok) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
+    int start = 0, cnt = 0;
+    if (ok) {
+      start = b.start_in ? b.start_in[i] + b.start_off : c.lens[s];
+      cnt = b.counts ? min(max(b.counts[i], 0), b.P) : b.P;
+      if (b.done && b.done[i]) cnt = 0;
+      else if (b.start_in) c.lens[s] = start;
+      if (start < 0 || cnt > c.max_events - start) {
+        if (cnt > 0) atomicOr(c.status, TPPSD_STATUS_CAPACITY);
+        cnt = 0;
+      }
+      need_sum += max(0, (cnt > 0 ? (start + cnt) / CACHE_BLOCK : 0) - c.held[s]);
+    }
+    c.p_seq[i] = ok ? s : -1;
+    c.p_start[i] = start;
+    c.p_count[i] = cnt;
+  }
+  int total;
+  int off = block_scan(need_sum, &total);
+  const int avail = total > 0 ? list_bits(c.freeb, c.n_pages, total, c.list) : 0;
+  int pages_sum = 0;
+  for (int i = i0; i < i1; ++i) {
+    const int s = c.p_seq[i];
+    if (s < 0) continue;
+    const int start = c.p_start[i];
+    int cnt = c.p_count[i];
+    const int held = c.held[s], need = max(0, (cnt > 0 ? (start + cnt) / CACHE_BLOCK : 0) - held);
+    if (need > 0) {
+      if (off + need <= avail) {
+        for (int j = 0; j < need; ++j) {
+          const int page = c.list[off + j];
+          c.table[(size_t)s * c.NP + held + j] = page;
+          c.refs[page] = 1;
+          atomicAnd(&c.freeb[page >> 5], ~(1u << (page & 31)));
+        }
+        c.held[s] = held + need;
+      } else {   // the rows before took the pages that were left
+        atomicOr(c.status, TPPSD_STATUS_PAGES);
+        c.p_count[i] = cnt = 0;
+      }
+      off += need;
+    }
+    c.pend[s] = cnt;
+    if (cnt > 0) {
+      const int top = (start + cnt - 1) / CACHE_BLOCK;
+      c.low[s] = max(top - 1, min(c.low[s], start / CACHE_BLOCK));
+      pages_sum += top;
+    }
+  }
+  // work items: equal page ranges over the batch, about split_target of them
+  int all_pages;
+  block_scan(pages_sum, &all_pages);
+  const int chunk = b.split_target > 0 ? max(4, (all_pages + b.split_target - 1) / b.split_target) : INT32_MAX;
+  int item_sum = 0;
+  auto splits = [&](int i) {
+    const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0;
+    return chunk == INT32_MAX || top <= chunk ? 1 : (top + chunk - 1) / chunk;
+  };
+  for (int i = i0; i < i1; ++i) item_sum += splits(i);
+  int n_items;
+  int at = block_scan(item_sum, &n_items);
+  for (int i = i0; i < i1; ++i) {
+    const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0, n = splits(i);
+    c.p_item[i] = at;
+    for (int j = 0; j < n; ++j) {
+      const int lo = n == 1 ? 0 : j * chunk, hi = n == 1 ? top : min(top, lo + chunk);
+      c.items[at++] = make_int4(i, lo, hi, j + 1 == n);
+    }
+  }
+  if (tid == 0) {
+    c.p_item[b.B] = n_items;
+    c.counts[0] = n_items;
+  }
+}
+
+__global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
+  const int i = blockIdx.x * blockDim.x + threadIdx.x;
+  if (i >= B) return;
+  const int s = c.p_seq[i], cnt = c.p_count[i];
+  if (s < 0 || cnt <= 0) return;
+  int n = c.p_start[i] + (accept ? min(max(accept[i], 0), cnt) : cnt);
+  if (n % CACHE_BLOCK && n / CACHE_BLOCK < c.low[s]) {   // the ring no longer holds the block that would be open
+    atomicOr(c.status, TPPSD_STATUS_OPEN);
+    n = n / CACHE_BLOCK * CACHE_BLOCK;
+  }
+  c.lens[s] = n;
+  c.pend[s] = 0;
+}
+
+__global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t *lens) {
+  __shared__ int range[2];
+  const int s = seqs[blockIdx.x];
+  if (threadIdx.x == 0) {
+    range[0] = range[1] = 0;
+    int n = lens ? lens[blockIdx.x] : 0;
+    if (s < 0 || s >= c.S || n < 0) {
+      atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
+    } else {
+      const int len = ld_agent(&c.lens[s]);
+      if (n >= len) {
+        n = len;
+      } else if (n % CACHE_BLOCK && n / CACHE_BLOCK < c.low[s]) {
+        atomicOr(c.status, TPPSD_STATUS_OPEN);
+        n = n / CACHE_BLOCK * CACHE_BLOCK;
+      }
+      // minima: a sequence that is named twice keeps the shorter length, and
+      // each of its pages is let go by one of the two
+      atomicMin(&c.lens[s], n);
+      range[0] = n / CACHE_BLOCK;
+      range[1] = atomicMin(&c.held[s], range[0]);
+      c.pend[s] = 0;
+    }
+  }
+  __syncthreads();
+  for (int j = range[0] + threadIdx.x; j < range[1]; j += blockDim.x) {
+    int32_t *e = &c.table[(size_t)s * c.NP + j];
+    page_drop(c, *e);
+    *e = -1;
+  }
+}
+
+// Which pairs of a fork or copy are carried out: both sequences exist, a
+// destination is named once (the first pair counts) and, within one cache, is
+// no pair's source. Verdicts into to.p_seq.
+__global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev from, int n, const int32_t *src,
+                                                         const int32_t *dst, int same) {
+  auto ok = [&](int i) { return src[i] >= 0 && src[i] < from.S && dst[i] >= 0 && dst[i] < to.S; };
+  for (int i = threadIdx.x; i < n; i += PLAN_NT)
+    if (ok(i)) {
+      st_agent(&to.owner[dst[i]], INT32_MAX);
+      if (same) {
+        st_agent(&to.role[dst[i]], 0);
+        st_agent(&to.role[src[i]], 0);
+      }
+    }
+  for (int w = threadIdx.x; w < (from.n_pages + 31) / 32 && !same; w += PLAN_NT) from.mark[w] = 0u;
+  __threadfence();
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += PLAN_NT)
+    if (ok(i)) {
+      atomicMin(&to.owner[dst[i]], i);
+      if (same) atomicOr(&to.role[src[i]], 1);
+    }
+  __threadfence();
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += PLAN_NT) {
+    bool good = ok(i) && ld_agent(&to.owner[dst[i]]) == i;
+    if (good && same) good = !ld_agent(&to.role[dst[i]]);
+    if (!good) atomicOr(to.status, TPPSD_STATUS_SEQUENCE);
+    if (good && from.lens[src[i]] > to.max_events) {
+      atomicOr(to.status, TPPSD_STATUS_CAPACITY);
+      good = false;
+    }
+    to.p_seq[i] = good ? 1 : 0;
+  }
+}
+
+// lets go what the destination holds, and (copies) marks the source's pages
+__device__ void dst_clear(const CacheDev &c, int d) {
+  const int held = c.held[d];
+  for (int j = threadIdx.x; j < held; j += blockDim.x) {
+    int32_t *e = &c.table[(size_t)d * c.NP + j];
+    page_drop(c, *e);
+    *e = -1;
+  }
+}
+
+// open rows of a source sequence (len mod 64 of them) into the destination's ring, 16 bytes a thread
+__device__ void copy_tail(const CacheDev &to, const CacheDev &from, int layer, int s, int d, int len) {
+  const int e = to.bf16 ? 2 : 4, open = len % CACHE_BLOCK, slot0 = len / CACHE_BLOCK * CACHE_BLOCK % CACHE_RING;
+  const int row16 = to.dh * e / 16, side16 = CACHE_RING * row16;   // 16-byte words
+  const uint4 *a = (const uint4 *)from.tails + ((size_t)layer * from.S + s) * to.KV * 2 * side16 + slot0 * row16;
+  uint4 *b = (uint4 *)to.tails + ((size_t)layer * to.S + d) * to.KV * 2 * side16 + slot0 * row16;
+  const int n = open * row16;
+  for (int i = threadIdx.x; i < to.KV * 2 * n; i += blockDim.x) {
+    const int side = i / n, j = i - side * n;
+    b[(size_t)side * side16 + j] = a[(size_t)side * side16 + j];
+  }
+}
+
+// grid (pairs, 1 + layers): table and counters, then each layer's open rows
+__global__ void k_cache_fork(CacheDev c, const int32_t *src, const int32_t *dst) {
+  const int i = blockIdx.x;
+  if (!c.p_seq[i]) return;
+  const int s = src[i], d = dst[i], len = c.lens[s], np = len / CACHE_BLOCK;
+  if (blockIdx.y > 0) {
+    copy_tail(c, c, blockIdx.y - 1, s, d, len);
+    return;
+  }
+  dst_clear(c, d);
+  __syncthreads();
+  for (int j = threadIdx.x; j < np; j += blockDim.x) {
+    const int page = c.table[(size_t)s * c.NP + j];
+    atomicAdd(&c.refs[page], 1);
+    c.table[(size_t)d * c.NP + j] = page;
+  }
+  if (threadIdx.x == 0) {
+    c.lens[d] = len;
+    c.held[d] = np;
+    c.low[d] = np;
+    c.pend[d] = 0;
+  }
+}
+
+__global__ void k_copy_mark(CacheDev to, CacheDev from, const int32_t *src, const int32_t *dst) {
+  const int i = blockIdx.x;
+  if (!to.p_seq[i]) return;
+  const int s = src[i], d = dst[i], np = from.lens[s] / CACHE_BLOCK;
+  dst_clear(to, d);
+  for (int j = threadIdx.x; j < np; j += blockDim.x) {
+    const int page = from.table[(size_t)s * from.NP + j];
+    atomicOr(&from.mark[page >> 5], 1u << (page & 31));
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) to.lens[d] = to.held[d] = to.low[d] = to.pend[d] = 0;
+}
+
+// the marked pages in ascending order get the destination's lowest free pages
+__global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev from) {
+  const int n = list_bits(from.mark, from.n_pages, from.n_pages, from.list);
+  const int avail = n > 0 ? list_bits(to.freeb, to.n_pages, n, to.list) : 0;
+  const bool fits = avail == n;
+  for (int k = threadIdx.x; k < n && fits; k += PLAN_NT) {
+    const int page = to.list[k];
+    from.map[from.list[k]] = page;
+    to.refs[page] = 0;
+    atomicAnd(&to.freeb[page >> 5], ~(1u << (page & 31)));
+  }
+  if (threadIdx.x == 0) {
+    to.counts[1] = fits ? n : -1;
+    if (!fits) atomicOr(to.status, TPPSD_STATUS_PAGES);
+  }
+}
+
+// grid.x = n (1 + L) workgroups for the sequences, the rest for the pages
+__global__ void k_copy_data(CacheDev to, CacheDev from, int n, const int32_t *src, const int32_t *dst) {
+  const int pages = to.counts[1];
+  if (pages < 0) return;
+  const int seq_wgs = n * (1 + to.L);
+  if ((int)blockIdx.x < seq_wgs) {
+    const int i = blockIdx.x % n, layer = (int)blockIdx.x / n - 1;
+    if (!to.p_seq[i]) return;
+    const int s = src[i], d = dst[i], len = from.lens[s], np = len / CACHE_BLOCK;
+    if (layer >= 0) {
+      copy_tail(to, from, layer, s, d, len);
+      return;
+    }
+    for (int j = threadIdx.x; j < np; j += blockDim.x) {
+      const int page = from.map[from.table[(size_t)s * from.NP + j]];
+      to.table[(size_t)d * to.NP + j] = page;
+      atomicAdd(&to.refs[page], 1);
+    }
+    if (threadIdx.x == 0) {
+      to.lens[d] = len;
+      to.held[d] = to.low[d] = np;
+    }
+    return;
+  }
+  const size_t words = to.KV * page_tile(to) / 16;   // 16-byte words of a page's layer
+  const size_t wgs = gridDim.x - seq_wgs;
+  for (size_t w = blockIdx.x - seq_wgs; w < (size_t)pages * to.L; w += wgs) {
+    const int layer = (int)(w / pages), k = (int)(w - (size_t)layer * pages);
+    const size_t a = (size_t)layer * from.n_pages + from.list[k], b = (size_t)layer * to.n_pages + to.list[k];
+    const uint4 *x = (const uint4 *)from.pages + a * words;
+    uint4 *y = (uint4 *)to.pages + b * words;
+    for (size_t j = threadIdx.x; j < words; j += blockDim.x) y[j] = x[j];
+    for (int j = threadIdx.x; j < 2 * to.KV; j += blockDim.x)
+      to.scales[b * 2 * to.KV + j] = from.scales[a * 2 * to.KV + j];
+  }
+}
+
+// ---- fragment order ---------------------------------------------------------
+// A (page, layer, head) tile is the keys' 64 dh codes, then the values'. The
+// attention reads both in 16-byte words, word c of lane l = 16 g + m at
+// c 1024 + 16 l:
+//   keys: fragment (tile t of 16 keys, k step s) holds key 16 t + m, columns
+//     32 s + 8 g .. + 7 (d_head 16: columns 4 g .. + 3 of the one step)
+//   values: fragment (column tile u, half w) holds column 16 u + m of the keys
+//     16 (2 w + (j >> 2)) + 4 g + (j & 3), j = 0..7: the keys whose scores that
+//     lane group holds after the S^T products of tiles 2 w and 2 w + 1
+// byte i of word c of lane l of the keys: (key, column)
+template <int DH> __device__ __forceinline__ void key_at(int c, int lane, int i, int &key, int &col) {
+  const int m = lane & 15, g = lane >> 4;
+  if (DH == 16) {
+    key = 16 * (i >> 2) + m;
+    col = 4 * g + (i & 3);
+  } else {
+    constexpr int NS = DH >= 32 ? DH / 32 : 1;
+    const int f = 2 * c + (i >> 3), t = f / NS, s = f - t * NS;
+    key = 16 * t + m;
+    col = 32 * s + 8 * g + (i & 7);
+  }
+}
+__device__ __forceinline__ void value_at(int c, int lane, int i, int &key, int &col) {
+  const int m = lane & 15, g = lane >> 4, w = i >> 3, j = i & 7;
+  key = 16 * (2 * w + (j >> 2)) + 4 * g + (j & 3);
+  col = 16 * c + m;
+}
+// where element (key, column) is
+template <int DH> __device__ __forceinline__ int key_byte(int key, int col) {
+  const int t = key >> 4, m = key & 15;
+  if (DH == 16) return (16 * (col >> 2) + m) * 16 + t * 4 + (col & 3);
+  constexpr int NS = DH >= 32 ? DH / 32 : 1;
+  const int f = t * NS + (col >> 5), g = (col >> 3) & 3;
+  return (f >> 1) * 1024 + (16 * g + m) * 16 + (f & 1) * 8 + (col & 7);
+}
+__device__ __forceinline__ int value_byte(int key, int col) {
+  const int t = key >> 4, g = (key >> 2) & 3;
+  return (col >> 4) * 1024 + (16 * g + (col & 15)) * 16 + (t >> 1) * 8 + (t & 1) * 4 + (key & 3);
+}
+
+template <typename ACT> __device__ __forceinline__ size_t v_off(const CacheRows &r, int i, int p, int h, int dh, int j) {
+  return r.v_blocked ? i * r.v_sb + h * r.v_sh + (size_t)(p >> 3) * 8 * dh + j * 8 + (p & 7)
+                     : i * r.v_sb + p * r.v_sp + h * r.v_sh + j;
+}
+
+// exponent of the scale for block maximum m (>= 0, finite): the least e with m <= 448 2^e
+__device__ __forceinline__ int scale_exp(float m) {
+  const uint32_t u = __float_as_uint(m);
+  if (m == 0.f) return 0;
+  // 448 = 1.75 2^8 (subnormal maxima fall under the least exponent anyway)
+  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return max(e, CACHE_E_MIN);
+}
+
+// x 2^-e as an e4m3 code; infinities and NaN become NaN
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+}
+
+// Appends to one layer. Grid (row, key/value head, block of positions that the
+// rows reach): the block's rows go through LDS; its new rows into the ring
+// where the ring keeps them (the last two blocks), and a block that becomes
+// whole is rounded to 8 bits and written as a page tile. Reads each new row
+// once and writes one byte per element of a whole block: bound by memory.
+template <typename ACT, int DH>
+__global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int P, CacheRows r) {
+  __shared__ ACT rows[2][CACHE_BLOCK][DH];
+  __shared__ float top[2][4];
+  const int i = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int s = c.p_seq[i], cnt = c.p_count[i], start = c.p_start[i];
+  if (s < 0 || cnt <= 0) return;
+  const int end = start + cnt, first = start / CACHE_BLOCK, last = (end - 1) / CACHE_BLOCK;
+  const int blk = first + blockIdx.z;
+  if (blk > last) return;
+  const int base = blk * CACHE_BLOCK, n = min(CACHE_BLOCK, end - base);
+  const int old = max(0, min(start - base, CACHE_BLOCK));   // rows of the block from before (first block only)
+  const bool whole = n == CACHE_BLOCK;
+  ACT *ring[2];
+#pragma unroll
+  for (int sd = 0; sd < 2; ++sd)
+    ring[sd] = (ACT *)c.tails + ((((size_t)layer * c.S + s) * c.KV + h) * 2 + sd) * CACHE_RING * DH;
+  const ACT *K = (const ACT *)r.k, *V = (const ACT *)r.v;
+  // element of a row from before the call's rows, or of the call's
+  auto k_new = [&](int pos, int j) { return K[i * r.k_sb + (size_t)(pos - start) * r.k_sp + h * r.k_sh + j]; };
+  auto v_new = [&](int pos, int j) { return V[v_off<ACT>(r, i, pos - start, h, DH, j)]; };
+  const bool keep = blk >= last - 1;
+  const bool need_old = whole || P > CACHE_BLOCK;
+  for (int x = tid; x < CACHE_BLOCK * DH; x += 256) {
+    const int row = x / DH, j = x - row * DH, pos = base + row, slot = pos % CACHE_RING;
+    ACT kv = 0, vv = 0;
+    if (row < old) {
+      if (need_old) kv = ring[0][slot * DH + j], vv = ring[1][slot * DH + j];
+    } else if (row < n) {
+      kv = k_new(pos, j);
+      vv = v_new(pos, j);
+    }
+    rows[0][row][j] = kv;
+    rows[1][row][j] = vv;
+  }
+  __syncthreads();
+  // the first block's slots may be those of a block that the ring keeps: that
+  // block's rows go in here, behind the reads of the old ones
+  const int later = (last - first) % 2 == 0 ? last : last - 1;
+  const bool shares = later > first && old > 0;
+  if (blk == first && P > CACHE_BLOCK && old > 0) {   // the attention of this call still needs the old rows
+    ACT *st = (ACT *)c.stash + ((size_t)i * c.KV + h) * 2 * CACHE_BLOCK * DH;
+    for (int x = tid; x < old * DH; x += 256) {
+      st[x] = (&rows[0][0][0])[x];
+      st[CACHE_BLOCK * DH + x] = (&rows[1][0][0])[x];
+    }
+  }
+  if (keep && !(shares && blk == later)) {
+    for (int x = tid + old * DH; x < n * DH; x += 256) {
+      const int slot0 = base % CACHE_RING;
+      ring[0][slot0 * DH + x] = (&rows[0][0][0])[x];
+      ring[1][slot0 * DH + x] = (&rows[1][0][0])[x];
+    }
+  }
+  if (blk == first && shares) {
+    const int b2 = later * CACHE_BLOCK, n2 = min(CACHE_BLOCK, end - b2);
+    for (int x = tid; x < n2 * DH; x += 256) {
+      const int row = x / DH, j = x - row * DH;
+      ring[0][(b2 % CACHE_RING + row) * DH + j] = k_new(b2 + row, j);
+      ring[1][(b2 % CACHE_RING + row) * DH + j] = v_new(b2 + row, j);
+    }
+  }
+  if (!whole) return;
+  // block maxima over finite elements
+  float m[2] = {0.f, 0.f};
+  for (int x = tid; x < CACHE_BLOCK * DH; x += 256)
+#pragma unroll
+    for (int sd = 0; sd < 2; ++sd) {
+      const float a = fabsf(ld((const ACT *)&rows[sd][0][0], x));
+      m[sd] = a < INFINITY ? fmaxf(m[sd], a) : m[sd];
+    }
+#pragma unroll
+  for (int sd = 0; sd < 2; ++sd) {
+    m[sd] = lanes_max(m[sd]);
+    if (lane == 0) top[sd][wave] = m[sd];
+  }
+  __syncthreads();
+  const size_t page = (size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk];
+  uint8_t *out = c.pages + (page * c.KV + h) * (2 * CACHE_BLOCK * DH);
+#pragma unroll
+  for (int sd = 0; sd < 2; ++sd) {
+    const int e = scale_exp(fmaxf(fmaxf(top[sd][0], top[sd][1]), fmaxf(top[sd][2], top[sd][3])));
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    if (tid == 0) c.scales[(page * c.KV + h) * 2 + sd] = __uint_as_float((uint32_t)(127 + e) << 23);
+    for (int x = tid; x < CACHE_BLOCK * DH / 16; x += 256) {   // 16-byte words
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float f[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          int key, col;
+          if (sd == 0) key_at<DH>(x >> 6, x & 63, 4 * q + z, key, col);
+          else value_at(x >> 6, x & 63, 4 * q + z, key, col);
+          f[z] = ld((const ACT *)&rows[sd][key][0], col);
+        }
+        w[q] = codes4(f[0], f[1], f[2], f[3], inv);
+      }
+      *(uint4 *)(out + sd * CACHE_BLOCK * DH + 16 * x) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// Rows first[i] .. first[i] + count - 1 of sequences, as the cache holds them:
+// whole blocks from their codes, the open block from the ring; positions past
+// the sequence are left as they were. Grid (row, head, 64 positions).
+template <typename ACT, int DH>
+__global__ __launch_bounds__(256) void k_cache_read(CacheDev c, int layer, const int32_t *seqs, const int32_t *first,
+                                                    int count, ACT *k, ACT *v) {
+  const int i = blockIdx.x, h = blockIdx.y, s = seqs ? seqs[i] : i;
+  if (s < 0 || s >= c.S) {
+    if (threadIdx.x == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
+    return;
+  }
+  const int end = c.lens[s] + c.pend[s], f = first ? first[i] : 0;
+  if (f < 0) {
+    if (threadIdx.x == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
+    return;
+  }
+  const ACT *ring = (const ACT *)c.tails + (((size_t)layer * c.S + s) * c.KV + h) * 2 * CACHE_RING * DH;
+  for (int x = threadIdx.x; x < 2 * CACHE_BLOCK * DH; x += 256) {
+    const int sd = x / (CACHE_BLOCK * DH), y = x - sd * CACHE_BLOCK * DH, row = blockIdx.z * CACHE_BLOCK + y / DH;
+    const int j = y % DH;
+    if (row >= count || row >= end - f) continue;
+    const int pos = f + row, blk = pos / CACHE_BLOCK;
+    ACT *out = (sd ? v : k) + (((size_t)i * count + row) * c.KV + h) * DH + j;
+    if ((blk + 1) * CACHE_BLOCK <= end) {
+      const size_t tile = ((size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk]) * c.KV + h;
+      const int key = pos % CACHE_BLOCK;
+      const uint32_t code = c.pages[tile * (2 * CACHE_BLOCK * DH) + sd * CACHE_BLOCK * DH +
+                                    (sd ? value_byte(key, j) : key_byte<DH>(key, j))];
+      st(out, 0, __builtin_amdgcn_cvt_f32_fp8(code, 0) * c.scales[tile * 2 + sd]);
+    } else {
+      *out = ring[(sd * CACHE_RING + pos % CACHE_RING) * DH + j];
+    }
+  }
+}
+
+template <typename F> void by_width(const CacheDev &c, F f) {
+  auto widths = [&](auto act) {
+    if (c.dh == 16) f(act, std::integral_constant<int, 16>{});
+    else if (c.dh == 32) f(act, std::integral_constant<int, 32>{});
+    else if (c.dh == 64) f(act, std::integral_constant<int, 64>{});
+    else f(act, std::integral_constant<int, 128>{});
+  };
+  if (c.bf16) widths(bf16_t{});
+  else widths(float{});
+}
+
+}  // namespace
+
+void launch_cache_reset(const CacheDev &c, hipStream_t st) {
+  const size_t n = std::max((size_t)c.S * c.NP, (size_t)c.n_pages);
+  k_cache_reset<<<(unsigned)std::min<size_t>((n + 255) / 256, 1024), 256, 0, st>>>(c);
+}
+
+void launch_cache_begin(const CacheDev &c, const CacheBegin &b, hipStream_t st) {
+  k_cache_begin<<<1, PLAN_NT, 0, st>>>(c, b);
+}
+
+void launch_cache_append(const CacheDev &c, int layer, int B, int P, const CacheRows &r, hipStream_t st) {
+  const dim3 grid(B, c.KV, (CACHE_BLOCK - 1 + P + CACHE_BLOCK - 1) / CACHE_BLOCK);
+  by_width(c, [&](auto act, auto w) {
+    k_cache_append<decltype(act), decltype(w)::value><<<grid, 256, 0, st>>>(c, layer, P, r);
+  });
+}
+
+void launch_cache_commit(const CacheDev &c, int B, const int32_t *accept, hipStream_t st) {
+  k_cache_commit<<<(B + 255) / 256, 256, 0, st>>>(c, B, accept);
+}
+
+void launch_cache_truncate(const CacheDev &c, int n, const int32_t *seqs, const int32_t *lens, hipStream_t st) {
+  k_cache_truncate<<<n, 256, 0, st>>>(c, seqs, lens);
+}
+
+void launch_cache_fork(const CacheDev &c, int n, const int32_t *src, const int32_t *dst, hipStream_t st) {
+  k_cache_pairs<<<1, PLAN_NT, 0, st>>>(c, c, n, src, dst, 1);
+  k_cache_fork<<<dim3(n, 1 + c.L), 256, 0, st>>>(c, src, dst);
+}
+
+void launch_cache_copy(const CacheDev &to, const CacheDev &from, int n, const int32_t *src, const int32_t *dst,
+                       hipStream_t st) {
+  k_cache_pairs<<<1, PLAN_NT, 0, st>>>(to, from, n, src, dst, 0);
+  k_copy_mark<<<n, 256, 0, st>>>(to, from, src, dst);
+  k_copy_plan<<<1, PLAN_NT, 0, st>>>(to, from);
+  k_copy_data<<<n * (1 + to.L) + 2048, 256, 0, st>>>(to, from, n, src, dst);
+}
+
+void launch_cache_read(const CacheDev &c, int layer, int n, const int32_t *seqs, const int32_t *first, int count,
+                       void *k, void *v, hipStream_t st) {
+  const dim3 grid(n, c.KV, (count + CACHE_BLOCK - 1) / CACHE_BLOCK);
+  by_width(c, [&](auto act, auto w) {
+    typedef decltype(act) ACT;
+    k_cache_read<ACT, decltype(w)::value><<<grid, 256, 0, st>>>(c, layer, seqs, first, count, (ACT *)k, (ACT *)v);
+  });
+}
+
+}  // namespace tppsd

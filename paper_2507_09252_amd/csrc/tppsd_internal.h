@@ -11,6 +11,11 @@ namespace tppsd {
 
 typedef uint16_t bf16_t;   // raw bfloat16 bits
 
+// host: records the calling thread's error message and returns `code`; the
+// pending HIP error as TPPSD_E_HIP, or TPPSD_OK
+int fail(int code, const char *fmt, ...);
+int hip_check(const char *what);
+
 // Where the P tokens of a block forward come from: token p of sequence b is
 // committed event (start[b] + start_off + p) for p < n_ev, otherwise draft
 // slot (dr_off + p - n_ev).

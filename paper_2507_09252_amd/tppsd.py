@@ -22,6 +22,8 @@ TPPSD_OK = 0
 PREC = {"fp32": 0, "bf16": 1}
 FLAG_BONUS = 1
 STATUS_CAPACITY, STATUS_NONFINITE, STATUS_AR_CAP = 1, 2, 4
+STATUS_PAGES, STATUS_SEQUENCE, STATUS_OPEN = 8, 16, 32
+CACHE_BLOCK, CACHE_RING = 64, 128
 
 ERRORS = {1: "TPPSD_E_ARG", 2: "TPPSD_E_CONFIG", 3: "TPPSD_E_WORKSPACE", 4: "TPPSD_E_ORDER", 5: "TPPSD_E_HIP"}
 
@@ -33,6 +35,9 @@ EXPORTS = [
     "tppsd_state_status", "tppsd_timing_enable", "tppsd_timing_read", "tppsd_last_error",
     "tppsd_poisson_fit", "tppsd_draft_poisson", "tppsd_sample_sd_poisson", "tppsd_prefill_window",
     "tppsd_read_loglik", "tppsd_verify_noalloc",
+    "tppsd_cache_bytes", "tppsd_cache_entry", "tppsd_cache_create", "tppsd_cache_destroy", "tppsd_cache_reset",
+    "tppsd_cache_begin", "tppsd_cache_append", "tppsd_cache_attend", "tppsd_cache_commit", "tppsd_cache_truncate",
+    "tppsd_cache_fork", "tppsd_cache_copy", "tppsd_cache_read", "tppsd_cache_status",
 ]
 
 
@@ -75,6 +80,15 @@ class AcceptBufC(ctypes.Structure):
     _fields_ = [(n, c_void_p) for n in ("L", "n_new", "k_new", "t_new", "tau_new", "ar_iter", "flags")]
 
 
+class CacheCfgC(ctypes.Structure):
+    _fields_ = [(n, c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "d_head", "prec", "max_seqs", "max_events",
+                                       "n_pages")]
+
+
+class CacheRowsC(ctypes.Structure):
+    _fields_ = [(n, c_void_p) for n in ("q", "k", "v", "o")] + [(n, c_int64) for n in ("ldq", "ldk", "ldv", "ldo")]
+
+
 _lib = None
 
 
@@ -114,6 +128,21 @@ def lib():
         "tppsd_sample_sd_poisson": (c_int, [c_void_p, c_int, c_void_p, c_int, P(c_int), c_void_p]),
         "tppsd_prefill_window": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p]),
         "tppsd_read_loglik": (c_int, [c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_bytes": (c_int, [P(CacheCfgC), P(c_size_t)]),
+        "tppsd_cache_entry": (c_int, [P(CacheCfgC), c_int, P(c_char_p), P(c_size_t)]),
+        "tppsd_cache_create": (c_int, [P(CacheCfgC), c_void_p, c_size_t, P(c_void_p)]),
+        "tppsd_cache_destroy": (None, [c_void_p]),
+        "tppsd_cache_reset": (c_int, [c_void_p, c_void_p]),
+        "tppsd_cache_begin": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_append": (c_int, [c_void_p, c_int, P(CacheRowsC), c_void_p]),
+        "tppsd_cache_attend": (c_int, [c_void_p, c_int, P(CacheRowsC), ctypes.c_float, c_int, c_void_p]),
+        "tppsd_cache_commit": (c_int, [c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_truncate": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_fork": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_copy": (c_int, [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+        "tppsd_cache_read": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p, c_void_p,
+                                     c_void_p]),
+        "tppsd_cache_status": (c_int, [c_void_p, c_void_p, P(c_uint32)]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -358,3 +387,162 @@ class State:
         t = TimingC()
         _check(lib().tppsd_timing_read(self.handle, ctypes.byref(t)))
         return {name: getattr(t, name) for name, _ in TimingC._fields_}
+
+
+# ---------------------------------------------------------------------------
+# 8-bit paged cache
+# ---------------------------------------------------------------------------
+
+class Cache:
+    """tppsd_cache over a torch-allocated workspace, emptied; methods map 1:1 to
+    the C ABI. Rows are tensors [B, n_new, heads, d_head] whose heads are
+    contiguous ([d_head] elements each) and whose rows of the batch are n_new
+    positions apart (a slice of a fused projection's output is taken as it is).
+    Index tensors are int32 on the cache's device.
+
+    pages, scales, tails, table, lens, refs: views of the cache's arrays."""
+
+    def __init__(self, n_layers: int, n_heads: int, n_kv_heads: int, d_head: int, prec: str, max_seqs: int,
+                 max_events: int, n_pages: int = 0, device="cuda"):
+        self.n_layers, self.n_heads, self.n_kv_heads, self.d_head = n_layers, n_heads, n_kv_heads, d_head
+        self.max_seqs, self.max_events = max_seqs, max_events
+        self.dtype = torch.bfloat16 if prec == "bf16" else torch.float32
+        cfg = CacheCfgC(n_layers, n_heads, n_kv_heads, d_head, PREC[prec], max_seqs, max_events, n_pages)
+        n = c_size_t()
+        _check(lib().tppsd_cache_bytes(ctypes.byref(cfg), ctypes.byref(n)))
+        self.ws = torch.zeros(n.value, dtype=torch.uint8, device=device)
+        h = c_void_p()
+        _check(lib().tppsd_cache_create(ctypes.byref(cfg), _ptr(self.ws), n.value, ctypes.byref(h)))
+        self.handle = h
+        np_ = (max_events + CACHE_BLOCK - 1) // CACHE_BLOCK
+        self.n_pages = n_pages or np_ * max_seqs
+        L, S, KV, dh, N = n_layers, max_seqs, n_kv_heads, d_head, self.n_pages
+        shapes = {"pages": (torch.uint8, (L, N, KV, 2 * CACHE_BLOCK * dh)), "scales": (torch.float32, (L, N, KV, 2)),
+                  "tails": (self.dtype, (L, S, KV, 2, CACHE_RING, dh)), "table": (torch.int32, (S, np_)),
+                  "lens": (torch.int32, (S,)), "refs": (torch.int32, (N,))}
+        for i in range(len(shapes)):
+            name, off = c_char_p(), c_size_t()
+            _check(lib().tppsd_cache_entry(ctypes.byref(cfg), i, ctypes.byref(name), ctypes.byref(off)))
+            dt, shape = shapes[name.value.decode()]
+            size = int(np.prod(shape)) * torch.empty(0, dtype=dt).element_size()
+            setattr(self, name.value.decode(), self.ws[off.value:off.value + size].view(dt).view(shape))
+        self.tppsd_cache_reset()
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.tppsd_cache_destroy(self.handle)
+            self.handle = None
+
+    def _call(self, fn, *args):
+        """The entry point on this cache's device and that device's current stream."""
+        dev = self.ws.device.index
+        if dev == torch.cuda.current_device():
+            _check(fn(*args, _stream()))
+        else:
+            with torch.cuda.device(dev):
+                _check(fn(*args, _stream()))
+
+    def _ints(self, t, n=None, what="index"):
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.device != self.ws.device or t.dim() != 1 or not t.is_contiguous():
+            raise TppsdError(1, f"{what} must be a contiguous int32 vector on {self.ws.device}")
+        if n is not None and t.numel() != n:
+            raise TppsdError(1, f"{what} has {t.numel()} elements, needs {n}")
+        return t
+
+    def _row(self, t, heads, what):
+        B, P = self._plan
+        if t.dtype != self.dtype or t.device != self.ws.device or tuple(t.shape) != (B, P, heads, self.d_head):
+            raise TppsdError(1, f"{what} must be {self.dtype} [{B}, {P}, {heads}, {self.d_head}] on {self.ws.device}")
+        ld = t.stride(1) if P > 1 else (t.stride(0) if B > 1 else heads * self.d_head)
+        if t.stride(3) != 1 or (heads > 1 and t.stride(2) != self.d_head) or (B > 1 and t.stride(0) != P * ld):
+            raise TppsdError(1, f"{what}: heads must be contiguous and rows evenly spaced")
+        return t.data_ptr(), ld
+
+    def tppsd_cache_reset(self):
+        self._call(lib().tppsd_cache_reset, self.handle)
+        self._plan = None
+
+    def tppsd_cache_begin(self, n_new: int, seqs: Optional[torch.Tensor] = None,
+                          counts: Optional[torch.Tensor] = None, batch: Optional[int] = None):
+        """batch: rows of the call (default: as many as seqs or counts has, or every sequence)."""
+        if batch is None:
+            batch = seqs.numel() if seqs is not None else counts.numel() if counts is not None else self.max_seqs
+        seqs, counts = self._ints(seqs, batch, "seqs"), self._ints(counts, batch, "counts")
+        self._call(lib().tppsd_cache_begin, self.handle, batch, n_new, _ptr(seqs), _ptr(counts))
+        self._plan = (batch, n_new)
+
+    def _planned(self):
+        if self._plan is None:
+            raise TppsdError(4, "call tppsd_cache_begin first")
+
+    def tppsd_cache_append(self, layer: int, k: torch.Tensor, v: torch.Tensor):
+        self._planned()
+        (kp, ldk), (vp, ldv) = self._row(k, self.n_kv_heads, "k"), self._row(v, self.n_kv_heads, "v")
+        r = CacheRowsC(None, kp, vp, None, 0, ldk, ldv, 0)
+        self._call(lib().tppsd_cache_append, self.handle, layer, ctypes.byref(r))
+
+    def tppsd_cache_attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                           out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                           sink: bool = False) -> torch.Tensor:
+        """scale: default 1 / sqrt(d_head); out: default a new tensor, zero where rows are left out."""
+        self._planned()
+        if out is None:
+            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+        (qp, ldq), (op, ldo) = self._row(q, self.n_heads, "q"), self._row(out, self.n_heads, "out")
+        (kp, ldk), (vp, ldv) = self._row(k, self.n_kv_heads, "k"), self._row(v, self.n_kv_heads, "v")
+        r = CacheRowsC(qp, kp, vp, op, ldq, ldk, ldv, ldo)
+        self._call(lib().tppsd_cache_attend, self.handle, layer, ctypes.byref(r),
+                                        self.d_head ** -0.5 if scale is None else scale, int(sink))
+        return out
+
+    def tppsd_cache_commit(self, accept: Optional[torch.Tensor] = None):
+        self._planned()
+        accept = self._ints(accept, self._plan[0], "accept")
+        self._call(lib().tppsd_cache_commit, self.handle, _ptr(accept))
+        self._plan = None
+
+    def tppsd_cache_truncate(self, seqs: torch.Tensor, lens: Optional[torch.Tensor] = None):
+        seqs = self._ints(seqs, None, "seqs")
+        lens = self._ints(lens, seqs.numel(), "lens")
+        self._call(lib().tppsd_cache_truncate, self.handle, seqs.numel(), _ptr(seqs), _ptr(lens))
+        self._plan = None
+
+    def tppsd_cache_fork(self, src: torch.Tensor, dst: torch.Tensor):
+        src = self._ints(src, None, "src")
+        dst = self._ints(dst, src.numel(), "dst")
+        self._call(lib().tppsd_cache_fork, self.handle, src.numel(), _ptr(src), _ptr(dst))
+        self._plan = None
+
+    def tppsd_cache_copy(self, source: "Cache", src: torch.Tensor, dst: torch.Tensor):
+        """Sequences src of the cache `source` into this cache's sequences dst."""
+        src = self._ints(src, None, "src")
+        dst = self._ints(dst, src.numel(), "dst")
+        if source.ws.device != self.ws.device:
+            raise TppsdError(1, "caches lie on different devices")
+        self._call(lib().tppsd_cache_copy, self.handle, source.handle, src.numel(), _ptr(src), _ptr(dst))
+        self._plan = None
+
+    def tppsd_cache_read(self, layer: int, first: Optional[torch.Tensor], count: int,
+                         k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                         seqs: Optional[torch.Tensor] = None):
+        """(k, v) [n, count, n_kv_heads, d_head] of positions first .. first + count - 1 (default 0)."""
+        n = seqs.numel() if seqs is not None else first.numel() if first is not None else self.max_seqs
+        first, seqs = self._ints(first, n, "first"), self._ints(seqs, n, "seqs")
+        shape = (n, count, self.n_kv_heads, self.d_head)
+        if k is None:
+            k = torch.zeros(shape, dtype=self.dtype, device=self.ws.device)
+        if v is None:
+            v = torch.zeros(shape, dtype=self.dtype, device=self.ws.device)
+        for t in (k, v):
+            if tuple(t.shape) != shape or t.dtype != self.dtype or t.device != self.ws.device or not t.is_contiguous():
+                raise TppsdError(1, f"outputs must be contiguous {self.dtype} {list(shape)}")
+        self._call(lib().tppsd_cache_read, self.handle, layer, n, _ptr(seqs), _ptr(first), count, _ptr(k), _ptr(v))
+        return k, v
+
+    def tppsd_cache_status(self) -> int:
+        bits = c_uint32()
+        with torch.cuda.device(self.ws.device):
+            _check(lib().tppsd_cache_status(self.handle, _stream(), ctypes.byref(bits)))
+        return bits.value

@@ -1,0 +1,475 @@
+"""The 8-bit paged cache against the float64 reference (cache_reference.py):
+appending, attention, forks, copies, truncation and what they refuse."""
+import numpy as np
+import pytest
+import torch
+
+from cache_reference import BLOCK, CAPACITY, OPEN, PAGES, RING, SEQUENCE, CacheRef, tolerance, values
+from paper_2507_09252_amd import tppsd as tp
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(v):
+    return torch.tensor(list(v), dtype=torch.int32, device="cuda")
+
+
+class Both:
+    """One cache in the library and in the reference, driven alike."""
+
+    def __init__(self, L, H, KV, dh, prec, S, max_events, n_pages=0, seed=0):
+        self.c = tp.Cache(L, H, KV, dh, prec, S, max_events, n_pages)
+        self.r = CacheRef(L, H, KV, dh, S, max_events, n_pages)
+        self.prec, self.rng = prec, np.random.default_rng(seed)
+
+    def rand(self, *shape, keys=False):
+        x = torch.from_numpy(self.rng.standard_normal(shape).astype(np.float32))
+        if keys:
+            x[..., ::5] *= 6.0
+        return x.to(self.c.dtype).cuda()
+
+    def begin(self, n_new, seqs=None, counts=None, batch=None):
+        B = batch or (len(seqs) if seqs is not None else len(counts) if counts is not None else self.r.S)
+        self.c.tppsd_cache_begin(n_new, None if seqs is None else ints(seqs), None if counts is None else ints(counts), B)
+        self.r.begin(B, n_new, seqs, counts)
+        self.B, self.P = B, n_new
+
+    def step(self, queries=True, sink=False, scale=None, rows=None):
+        """Appends random (or the given) rows to every layer, with or without attention, and compares the output."""
+        r = self.r
+        for layer in range(r.L):
+            if rows is not None:
+                q, k, v = rows[layer]
+            else:
+                k, v = self.rand(self.B, self.P, r.KV, r.dh, keys=True), self.rand(self.B, self.P, r.KV, r.dh)
+                q = self.rand(self.B, self.P, r.H, r.dh)
+            r.append(layer, values(k), values(v))
+            if not queries:
+                self.c.tppsd_cache_append(layer, k, v)
+                continue
+            out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+            self.c.tppsd_cache_attend(layer, q, k, v, out, scale, sink)
+            want = np.full(q.shape, 7.0)
+            f32scale = float(np.float32(r.dh ** -0.5 if scale is None else scale))
+            weight, score = r.attend(layer, values(q), want, f32scale, sink)
+            keys = int(max((st + n for _, st, n in r.plan), default=0))
+            tol = tolerance(self.prec, r.dh, keys, want, weight, score)
+            got = values(out)
+            bad = ~(np.abs(got - want) <= tol) & ~(np.isnan(got) & np.isnan(want))
+            assert not bad.any(), (layer, np.argwhere(bad)[:5], got[bad][:5], want[bad][:5], tol[bad][:5])
+
+    def commit(self, accept=None):
+        self.c.tppsd_cache_commit(None if accept is None else ints(accept))
+        self.r.commit(accept)
+
+    def same(self, status=None):
+        """Bookkeeping, status and every row that the cache holds."""
+        r, c = self.r, self.c
+        assert np.array_equal(c.lens.cpu().numpy(), r.lens)
+        assert np.array_equal(c.table.cpu().numpy(), r.table)
+        assert np.array_equal(c.refs.cpu().numpy(), r.refs)
+        bits = c.tppsd_cache_status()
+        assert bits == r.status, (bits, r.status)
+        if status is not None:
+            assert bits == status
+        n = int((r.lens + r.pend).max())
+        if n == 0:
+            return
+        for layer in range(r.L):
+            k, v = c.tppsd_cache_read(layer, None, n)
+            for side, got in ((0, values(k)), (1, values(v))):
+                for s in range(r.S):
+                    end = int(r.lens[s] + r.pend[s])
+                    assert np.array_equal(got[s, :end], r.held_rows(s, side, layer, end), equal_nan=True), (layer, side, s)
+                    assert not got[s, end:].any()
+
+
+# (precision, query heads, key/value heads, d_head)
+HEADS = [("bf16", 8, 8, 64), ("bf16", 4, 4, 32), ("bf16", 2, 2, 16), ("bf16", 8, 2, 128), ("bf16", 6, 1, 32),
+         ("fp32", 4, 4, 16), ("fp32", 2, 2, 32), ("fp32", 6, 2, 64), ("fp32", 2, 1, 128)]
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=lambda h: "-".join(map(str, h)))
+@pytest.mark.parametrize("P", [1, 5, 17, 33, 64])
+def test_attend_after_ragged_histories(heads, P):
+    """Steps of P positions after histories of 0 to 200 positions: into empty
+    sequences, up to, over and from block borders."""
+    prec, H, KV, dh = heads
+    lens = [0, 1, 63, 64, 65, 127, 128, 130, 200]
+    b = Both(2, H, KV, dh, prec, len(lens), 400, seed=P)
+    b.begin(max(lens), counts=lens)
+    b.step(queries=False)
+    b.commit()
+    b.same(0)
+    b.begin(P)
+    b.step(sink=P == 17)
+    b.same(0)
+    b.commit([P - i % (P + 1) for i in range(len(lens))])
+    b.begin(P, counts=[(i * 7) % (P + 1) for i in range(len(lens))])
+    b.step()
+    b.commit()
+    b.same(0)
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=lambda h: "-".join(map(str, h)))
+def test_attend_chunks(heads):
+    """Chunks of more than a block, of odd lengths, at odd starts."""
+    prec, H, KV, dh = heads
+    b = Both(1, H, KV, dh, prec, 3, 700, seed=3)
+    for P, counts in ((65, [65, 1, 0]), (131, [131, 130, 64]), (200, [200, 129, 191]), (97, [3, 97, 70])):
+        b.begin(P, counts=counts)
+        b.step(sink=P == 97)
+        b.commit()
+        b.same(0)
+
+
+@pytest.mark.parametrize("prec,H,KV,dh,B,n,P", [("bf16", 2, 2, 64, 1, 5000, 3), ("bf16", 8, 1, 128, 2, 2100, 1),
+                                                ("fp32", 2, 2, 16, 1, 3000, 33), ("bf16", 16, 2, 32, 1, 1500, 30),
+                                                ("bf16", 4, 4, 64, 70, 300, 129)])
+def test_attend_long(prec, H, KV, dh, B, n, P):
+    """Long contexts, whose pages are split over workgroups, groups of more than 64 query rows, many rows."""
+    b = Both(1, H, KV, dh, prec, B, n + 2 * P, seed=n)
+    b.begin(n, counts=[n - 37 * i % 200 for i in range(B)])
+    b.step(queries=False)
+    b.commit()
+    b.begin(P)
+    if B > 4:   # (the reference takes its time: four sequences' outputs)
+        r, keep = b.r, [0, 1, 35, 69]
+        k, v, q = b.rand(B, P, KV, dh), b.rand(B, P, KV, dh), b.rand(B, P, H, dh)
+        r.append(0, values(k), values(v))
+        got, want = values(b.c.tppsd_cache_attend(0, q, k, v)), np.zeros((B, P, H, dh))
+        r.plan = [x if i in keep else (-1, 0, 0) for i, x in enumerate(r.plan)]
+        weight, score = r.attend(0, values(q), want, dh ** -0.5, False)
+        assert (np.abs(got - want) <= tolerance(prec, dh, n + P, want, weight, score))[keep].all()
+        return
+    b.step()
+    b.commit()
+    b.same(0)
+
+
+@pytest.mark.parametrize("prec,dh", [("bf16", 64), ("fp32", 32), ("bf16", 128)])
+def test_chunking_does_not_matter(prec, dh):
+    """The same rows in one chunk, in chunks of 16, 37, 64 and 100, and one by
+    one: the same pages, scales and rows, and outputs of the same function."""
+    n, H = 300, 2
+    rng = np.random.default_rng(0)
+    q, k, v = (torch.from_numpy(rng.standard_normal((1, n, H, dh)).astype(np.float32)).to(
+        torch.bfloat16 if prec == "bf16" else torch.float32).cuda() for _ in range(3))
+    first = None
+    for chunk in (n, 100, 64, 37, 16, 1):
+        c = tp.Cache(1, H, H, dh, prec, 1, n)
+        out = []
+        for a in range(0, n, chunk):
+            x = slice(a, min(n, a + chunk))
+            c.tppsd_cache_begin(x.stop - a)
+            out.append(c.tppsd_cache_attend(0, q[:, x].contiguous(), k[:, x].contiguous(), v[:, x].contiguous()))
+            c.tppsd_cache_commit()
+        out = torch.cat(out, 1)
+        held = c.tppsd_cache_read(0, None, n)
+        if first is None:
+            first = (out, held, c)
+            continue
+        assert torch.equal(c.pages, first[2].pages) and torch.equal(c.scales, first[2].scales)
+        assert torch.equal(held[0], first[1][0]) and torch.equal(held[1], first[1][1])
+        # two kernels within the bound of the definition each: twice its 3 x 2^-8 (2^-16 for fp32) of |V| < 6
+        assert (out - first[0]).abs().max() < 2 * 6 * 3 * (2.0 ** -8 if prec == "bf16" else 2.0 ** -16)
+
+
+def test_scales_and_codes():
+    """Blocks of zeros, of one value, at the edges of a scale's range, tiny and
+    huge ones, and elements that are not finite."""
+    b = Both(1, 2, 2, 32, "fp32", 8, 64)
+    k = torch.zeros(8, 64, 2, 32)
+    gen = torch.Generator().manual_seed(1)
+    k[1] = 1.0
+    k[2] = torch.randn(64, 2, 32, generator=gen)
+    k[2, 5, 0, 3] = 448.0                       # the scale's own edge, and just past it
+    k[2, 5, 1, 3] = float(np.nextafter(np.float32(448), np.float32(449)))
+    k[3] = torch.randn(64, 2, 32, generator=gen) * 1e-30
+    k[4] = torch.randn(64, 2, 32, generator=gen) * 1e37
+    k[5] = torch.randn(64, 2, 32, generator=gen) * torch.exp2(torch.randint(-30, 8, (64, 2, 32), generator=gen).float())
+    k[6] = torch.randn(64, 2, 32, generator=gen)
+    k[6, 0, 0, 0], k[6, 1, 0, 1], k[6, 2, 1, 2] = float("nan"), float("inf"), float("-inf")
+    k[7] = torch.randn(64, 2, 32, generator=gen) * 2.0 ** -128     # subnormal fp32
+    k = k.cuda()
+    b.begin(64)
+    b.step(queries=False, rows=[(None, k, k.flip(0).contiguous())])
+    b.commit()
+    b.same(0)
+
+
+@pytest.mark.parametrize("prec,dh,start,P", [("bf16", 64, 0, 40), ("bf16", 32, 50, 33), ("fp32", 16, 60, 20),
+                                             ("bf16", 64, 30, 150), ("fp32", 64, 10, 140)])
+def test_not_finite_rows_reach_only_those_who_see_them(prec, dh, start, P):
+    b = Both(1, 2, 2, dh, prec, 2, 300, seed=5)
+    if start:
+        b.begin(start)
+        b.step(queries=False)
+        b.commit()
+    b.begin(P)
+    q, k, v = b.rand(2, P, 2, dh), b.rand(2, P, 2, dh), b.rand(2, P, 2, dh)
+    bad, kbad = P // 2, P - 2
+    v[0, bad, 0, 3], v[0, bad + 1, 0, 5], v[0, bad + 1, 1, 2] = float("nan"), float("inf"), float("-inf")
+    k[0, kbad, 0, 1] = float("nan")
+    out = b.c.tppsd_cache_attend(0, q, k, v)
+    fine_v, fine_k = torch.where(torch.isfinite(v), v, 0.0), torch.where(torch.isfinite(k), k, 0.0)
+    b.r.append(0, values(fine_k), values(fine_v))
+    # the codes of whole blocks are those of the finite elements
+    want = np.zeros((2, P, 2, dh))
+    weight, score = b.r.attend(0, values(q), want, float(np.float32(dh ** -0.5)), False)
+    got = values(out)
+    tol = tolerance(prec, dh, start + P, want, weight, score)
+    nan = np.zeros(want.shape, bool)
+    nan[0, bad:, 0, 3] = nan[0, bad + 1:, 0, 5] = nan[0, bad + 1:, 1, 2] = True
+    nan[0, kbad:, 0] = True
+    assert np.array_equal(~np.isfinite(got), nan), np.argwhere(~np.isfinite(got) != nan)[:8]
+    assert (np.abs(got - want)[~nan] <= tol[~nan]).all()
+
+
+def test_masked_scores_of_lowest_value_and_large_scale():
+    """Scores far below and above zero: the running maximum keeps the weights exact."""
+    b = Both(1, 2, 2, 32, "fp32", 2, 300, seed=9)
+    for n, f in ((100, 30.0), (64, -30.0), (70, 1.0)):
+        b.begin(n)
+        k = b.rand(2, n, 2, 32) + f
+        b.step(rows=[(b.rand(2, n, 2, 32) + 1.0, k, b.rand(2, n, 2, 32))], scale=2.5, sink=n == 70)
+        b.commit()
+    b.same(0)
+
+
+def test_rows_taken_from_a_fused_projection():
+    H, KV, dh, B, P = 4, 2, 64, 3, 9
+    b = Both(1, H, KV, dh, "bf16", B, 100)
+    x = b.rand(B, P, (H + 2 * KV + 1) * dh)
+    b.begin(P)
+    q, k, v = (x[..., a * dh:e * dh].unflatten(-1, (e - a, dh)) for a, e in ((0, H), (H, H + KV), (H + KV, H + 2 * KV)))
+    b.step(rows=[(q, k, v)])
+    out = q                                     # over the queries themselves
+    want = b.c.tppsd_cache_attend(0, q.clone(), k, v)
+    b.c.tppsd_cache_attend(0, q, k, v, out=out)
+    assert torch.equal(out, want)
+    b.commit()
+    b.same(0)
+
+
+def test_left_out_rows():
+    """Sequences that do not exist, named twice, past the capacity, without pages: nothing of them changes."""
+    b = Both(1, 2, 2, 16, "bf16", 6, 200, n_pages=4, seed=2)
+    b.begin(100, counts=[100, 100, 0, 30, 64, 5])
+    b.step()
+    b.same(0)
+    b.commit()
+    b.begin(20, seqs=[3, 6, -1, 3, 0, 2])
+    b.step()
+    b.same(SEQUENCE)
+    b.commit()
+    b.begin(101, seqs=[1, 0, 3, 4, 5], counts=[100, 101, 20, 1, 0])   # 0: 221 > 200; the last page goes to 1 ...
+    b.step()
+    b.commit()
+    b.same(SEQUENCE | CAPACITY | PAGES)
+    b.c.tppsd_cache_reset()
+    b.r = CacheRef(1, 2, 2, 16, 6, 200, 4)
+    b.same(0)
+
+
+def test_truncate_and_uncommitted_rows():
+    b = Both(2, 2, 1, 32, "bf16", 5, 500, seed=4)
+    b.begin(300, counts=[300, 299, 64, 10, 0])
+    b.step(queries=False)
+    b.commit()
+    b.c.tppsd_cache_truncate(ints([0, 1, 3]), ints([290, 128, 900]))
+    b.r.truncate([0, 1, 3], [290, 128, 900])
+    b.same(0)
+    b.begin(33)
+    b.step()
+    b.commit([0, 33, 5, 1, 2])
+    b.begin(70, seqs=[1, 0])
+    b.step()
+    b.commit([10, 0])
+    b.same(0)
+    b.c.tppsd_cache_truncate(ints([0, 2, 9, 4]), ints([100, 3, 1, -1]))   # inside a block that left the ring
+    b.r.truncate([0, 2, 9, 4], [100, 3, 1, -1])
+    b.same(SEQUENCE | OPEN)
+    b.begin(40)
+    b.step()
+    b.commit()
+    b.begin(400, counts=[0, 200, 0, 0, 0])
+    b.step()
+    b.commit([0, 20, 0, 0, 0])                                            # keeps less than the last two blocks
+    b.same(SEQUENCE | OPEN)
+    b.begin(3)
+    b.step()
+    b.commit()
+    b.c.tppsd_cache_truncate(ints([0, 0, 1, 2, 3, 4]))
+    b.r.truncate([0, 0, 1, 2, 3, 4])
+    b.same()
+    assert not b.r.refs.any()
+
+
+@pytest.mark.parametrize("prec,dh", [("bf16", 64), ("fp32", 16)])
+def test_forks_go_their_own_ways(prec, dh):
+    b = Both(2, 2, 2, dh, prec, 6, 400, seed=6)
+    b.begin(200, counts=[200, 190, 128, 60, 0, 33])
+    b.step(queries=False)
+    b.commit()
+    for src, dst in (([0, 0, 1], [4, 5, 3]), ([4, 3], [0, 1]), ([2, 2, 2], [0, 5, 1])):
+        b.c.tppsd_cache_fork(ints(src), ints(dst))
+        b.r.fork(src, dst)
+        b.same(0)
+        b.begin(70, counts=[70, 3, 65, 0, 64, 17])
+        b.step()
+        b.commit([70, 2, 65, 0, 3, 17])
+        b.same(0)
+    # itself, twice the same destination, a destination that is a source, none
+    src, dst = [0, 1, 2, 3, 7, 1], [0, 4, 4, 1, 2, -2]
+    b.c.tppsd_cache_fork(ints(src), ints(dst))
+    b.r.fork(src, dst)
+    b.same(SEQUENCE)
+
+
+def test_copies_compact_and_keep_sharing():
+    L, KV, dh = 2, 2, 32
+    a = Both(L, 2, KV, dh, "bf16", 7, 400, seed=7)
+    a.begin(330, counts=[330, 64, 128, 200, 5, 0, 300])
+    a.step(queries=False)
+    a.commit()
+    a.c.tppsd_cache_fork(ints([0, 0]), ints([2, 5]))
+    a.r.fork([0, 0], [2, 5])
+    b = Both(L, 2, KV, dh, "bf16", 6, 380, n_pages=10, seed=8)
+    b.begin(64, counts=[64, 0, 0, 64, 0, 0])
+    b.step(queries=False)
+    b.commit()
+    src, dst = [0, 2, 6, 4, 0], [1, 0, 5, 2, 4]              # 5 + 4 pages, one of which 0's own gave back
+    b.c.tppsd_cache_copy(a.c, ints(src), ints(dst))
+    b.r.copy(a.r, src, dst)
+    b.same(0)
+    a.same(0)
+    b.begin(17)
+    b.step()
+    b.commit()
+    b.same(0)
+    src, dst = [3, 9, 3, 6], [3, 0, 3, 6]                    # bad pairs stay out
+    b.c.tppsd_cache_copy(a.c, ints(src), ints(dst))
+    b.r.copy(a.r, src, dst)
+    b.same()
+    assert b.r.status & SEQUENCE
+    small = Both(L, 2, KV, dh, "bf16", 2, 380, n_pages=5, seed=8)
+    for src, dst in (([0], [1]), ([0, 6], [1, 0])):          # the second does not fit: both end empty
+        small.c.tppsd_cache_copy(a.c, ints(src), ints(dst))
+        small.r.copy(a.r, src, dst)
+        small.same()
+    assert small.r.status == PAGES and not small.r.lens.any()
+    short = Both(L, 2, KV, dh, "bf16", 2, 100, seed=8)
+    short.c.tppsd_cache_copy(a.c, ints([0, 1]), ints([0, 1]))
+    short.r.copy(a.r, [0, 1], [0, 1])
+    short.same(CAPACITY)
+
+
+def test_random_calls():
+    """A few hundred random calls on two caches: bookkeeping after each, rows and outputs along the way."""
+    rng = np.random.default_rng(11)
+    caches = [Both(1, 2, 1, 16, "bf16", 9, 350, n_pages=30, seed=1), Both(1, 2, 1, 16, "bf16", 5, 300, n_pages=17, seed=2)]
+    for turn in range(120):
+        x = rng.integers(2)
+        b, o = caches[x], caches[1 - x]
+        S, op = b.r.S, rng.choice(["step", "step", "step", "fork", "truncate", "copy"])
+        n = int(rng.integers(1, S + 1))
+        if op == "step":
+            P = int(rng.choice([1, 4, 20, 64, 90, 150]))
+            b.begin(P, seqs=rng.permutation(S)[:n].tolist(), counts=rng.integers(0, P + 1, n).tolist())
+            b.step(queries=turn % 3 == 0)
+            b.commit([int(max(0, c - rng.integers(0, 5))) for _, _, c in b.r.plan])
+        elif op == "fork":
+            src, dst = rng.integers(0, S, n).tolist(), rng.integers(0, S, n).tolist()
+            b.c.tppsd_cache_fork(ints(src), ints(dst))
+            b.r.fork(src, dst)
+        elif op == "truncate":
+            seqs = rng.permutation(S)[:n].tolist()
+            lens = rng.integers(0, 350, n).tolist()
+            b.c.tppsd_cache_truncate(ints(seqs), ints(lens))
+            b.r.truncate(seqs, lens)
+        else:
+            src, dst = rng.integers(0, o.r.S, n).tolist(), rng.permutation(S)[:n].tolist()
+            b.c.tppsd_cache_copy(o.c, ints(src), ints(dst))
+            b.r.copy(o.r, src, dst)
+        b.same()
+    for b in caches:
+        assert sorted(set(b.r.table[b.r.table >= 0])) == sorted(np.nonzero(b.r.refs)[0])
+
+
+def test_pages_past_four_gigabytes():
+    KV, dh, n = 8, 128, 40000                    # 128 KB of codes a page
+    b = tp.Cache(1, KV, KV, dh, "bf16", 2, (n - 8) * BLOCK, n)
+    b.tppsd_cache_begin((n - 8) * BLOCK, counts=ints([(n - 8) * BLOCK, 0]))   # takes the pages, brings no rows
+    b.tppsd_cache_commit()
+    x = Both(1, KV, KV, dh, "bf16", 1, 400, seed=12)
+    x.begin(200)
+    q, k, v = (x.rand(1, 200, KV, dh) for _ in range(3))
+    x.step(rows=[(q, k, v)])
+    b.tppsd_cache_begin(200, seqs=ints([1]))
+    out = b.tppsd_cache_attend(0, q, k, v)
+    b.tppsd_cache_commit()
+    assert b.table[1, :3].tolist() == [n - 8, n - 7, n - 6]
+    assert torch.equal(out, x.c.tppsd_cache_attend(0, q, k, v))
+    got, want = b.tppsd_cache_read(0, None, 200, seqs=ints([1])), x.c.tppsd_cache_read(0, None, 200)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert b.tppsd_cache_status() == 0
+
+
+def test_captured_steps_replay():
+    """begin, attend and commit captured once: every replay goes on from the device's counters."""
+    L, H, dh, B, P = 2, 2, 64, 3, 9
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    rows = [torch.randn(3, L, B, P, H, dh, generator=gen, device="cuda").bfloat16() for _ in range(30)]
+    q, k, v = (torch.empty(L, B, P, H, dh, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    out, accept = torch.zeros_like(q), ints([9, 8, 5])
+    caches = [tp.Cache(L, H, H, dh, "bf16", B, 400) for _ in range(2)]
+
+    def step(c):
+        c.tppsd_cache_begin(P, batch=B)
+        for layer in range(L):
+            c.tppsd_cache_attend(layer, q[layer], k[layer], v[layer], out[layer])
+        c.tppsd_cache_commit(accept)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        step(caches[1])
+    torch.cuda.current_stream().wait_stream(side)
+    caches[1].tppsd_cache_reset()
+    for x in rows:
+        for a, t in zip((q, k, v), x):
+            a.copy_(t)
+        out.zero_()
+        step(caches[0])
+        want = out.clone()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        assert torch.equal(caches[0].lens, caches[1].lens) and torch.equal(caches[0].table, caches[1].table)
+    assert caches[0].lens.tolist() == [270, 240, 150]
+    assert torch.equal(caches[0].pages, caches[1].pages) and torch.equal(caches[0].tails, caches[1].tails)
+
+
+def test_other_stream():
+    b, s = Both(1, 2, 2, 64, "bf16", 2, 200), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for P in (100, 1, 30):
+            b.begin(P)
+            b.step()
+            b.commit()
+        b.same(0)
+
+
+def test_results_repeat():
+    """The same calls give the same bits, with the keys split over workgroups too."""
+    outs = []
+    for _ in range(3):
+        b = Both(1, 2, 2, 64, "bf16", 2, 3000, seed=3)
+        b.begin(2900)
+        b.c.tppsd_cache_append(0, b.rand(2, 2900, 2, 64), b.rand(2, 2900, 2, 64))
+        b.c.tppsd_cache_commit()
+        b.c.tppsd_cache_begin(5)
+        outs.append(b.c.tppsd_cache_attend(0, *(b.rand(2, 5, 2, 64) for _ in range(3))))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
