@@ -63,6 +63,12 @@ extern "C" {
                                  distribution of §2.3). Off: the round yields the
                                  gamma drafts (Algorithm 1 as printed).          */
 
+#define TPPSD_FLAG_CACHE8 2u /* the target's keys and values in an 8-bit paged cache
+                                (below: tppsd_cache_*), half the bytes of bf16. Prefill,
+                                verify passes and AR steps read it alike, so TPP-SD
+                                keeps the law of AR sampling with this cache. The
+                                workspace is tppsd_state_bytes_flags's. */
+
 /* ---- sticky device status bits (tppsd_state_status) ----------------------- */
 #define TPPSD_STATUS_CAPACITY  1u  /* an append would pass max_events           */
 #define TPPSD_STATUS_NONFINITE 2u  /* a log-density or sampled interval was NaN/Inf */
@@ -175,6 +181,11 @@ void tppsd_model_destroy(tppsd_model *m);
 int tppsd_state_bytes(const tppsd_model *target, const tppsd_model *draft, int B,
                       int max_events, int max_gamma, size_t *bytes);
 
+/* tppsd_state_bytes for a state of these flags (TPPSD_FLAG_CACHE8 has a
+ * workspace of its own). Errors: as tppsd_state_bytes, unknown flags: TPPSD_E_ARG. */
+int tppsd_state_bytes_flags(const tppsd_model *target, const tppsd_model *draft, int B, int max_events,
+                            int max_gamma, unsigned flags, size_t *bytes);
+
 /* Creates a sampler state in the caller's workspace (256-byte aligned,
  * tppsd_state_bytes or more; a workspace short of prefill rows alone is also
  * taken, and its prefill then runs in the longest chunks, of 16 positions or a
@@ -207,6 +218,24 @@ int tppsd_prefill(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, 
  * tppsd_prefill. */
 int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, int n_gen,
                          const float *d_t_end, hipStream_t stream);
+
+/* Continues generation runs: sequence b of `to` becomes a copy of sequence
+ * d_parent[b] (device, [to's B]) of `from` - events, counters, end time,
+ * log-likelihood and caches - and goes on independently. With to == from
+ * (resampling particles), a sequence that is its own parent stays as it is and
+ * a parent has to be one; with another state (many continuations of few encoded
+ * histories, or a job that needs more room), which is of the same models and
+ * cache flag and takes over from's n_gen, every sequence is replaced, its
+ * accounting starts at zero and its draws are those of its own seed. 8-bit
+ * caches share (to == from) or copy once pages that several sequences have. A
+ * sequence whose parent does not exist, is not its own (to == from) or has
+ * more events than to's max_events is left as it is (to == from) or empty and
+ * finished (TPPSD_STATUS_SEQUENCE). Within a state a copy draws from counters
+ * that neither it nor its parent has used, for up to 4095 forks of a run.
+ * Errors: TPPSD_E_ARG (null, from's history length + n_gen + to's
+ * max_gamma + 1 > to's max_events), TPPSD_E_CONFIG (models or TPPSD_FLAG_CACHE8
+ * differ), TPPSD_E_ORDER (from has no prefill), TPPSD_E_HIP. */
+int tppsd_state_fork(tppsd_state *to, tppsd_state *from, const int32_t *d_parent, hipStream_t stream);
 
 /* Drafting (§4.3 "Drafting", Algorithm 1's inner loop): gamma sequential draws
  * from the draft model for every unfinished sequence, using the Philox
@@ -469,7 +498,7 @@ int tppsd_cache_truncate(tppsd_cache *c, int n, const int32_t *d_seqs, const int
  * whole pages are shared (they are never written again) and the open block's
  * rows copied. A source may be named many times; a pair whose destination
  * another pair names before it or as a source is left out
- * (TPPSD_STATUS_SEQUENCE). Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+ * (TPPSD_STATUS_SEQUENCE); a pair of two negative numbers is none. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
 int tppsd_cache_fork(tppsd_cache *c, int n, const int32_t *d_src, const int32_t *d_dst, hipStream_t stream);
 
 /* Sequences d_dst[j] of `to` become copies of sequences d_src[j] of `from`, in

@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libtppsd.so")
 ARCH = "gfx950"
 
 DEVICE_SRCS = ("tppsd_kernels.hip", "tppsd_attention.hip", "tppsd_poisson.hip", "tppsd_draft_rows.hip",
-               "tppsd_draft_regs.hip", "tppsd_cache.hip", "tppsd_cache_attn.hip")
+               "tppsd_draft_regs.hip", "tppsd_cache.hip", "tppsd_cache_attn.hip", "tppsd_fork.hip")
 HOST_SRCS = ("tppsd.cpp", "tppsd_cache.cpp")
 
 HIPCC_FLAGS = [

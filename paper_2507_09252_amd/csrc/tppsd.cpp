@@ -21,6 +21,7 @@
 #include <vector>
 
 #include "../../include/tppsd.h"
+#include "tppsd_cache.h"
 #include "tppsd_internal.h"
 
 using namespace tppsd;
@@ -57,6 +58,8 @@ void drop_graph(hipGraphExec_t *g) {
   if (*g) (void)hipGraphExecDestroy(*g);
   *g = nullptr;
 }
+
+constexpr unsigned STATE_FLAGS = TPPSD_FLAG_BONUS | TPPSD_FLAG_CACHE8;
 
 constexpr size_t ALIGN = 256;
 inline size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
@@ -235,6 +238,11 @@ struct tppsd_state {
   float *t_end = nullptr;    // [B] end times (+inf: none)
   double *ll = nullptr;      // [B] model log-likelihood of the generated events
   ModelCache cT, cD;
+  // TPPSD_FLAG_CACHE8: the target's keys and values (cT then has no slabs), and
+  // a pass's new rows on their way there, [B][H][kv_stride(P)][dh] as in a slab
+  bool cache8 = false;
+  CacheDev c8{};
+  char *k_new = nullptr, *v_new = nullptr;
   // activation scratch
   float *x = nullptr;
   void *a = nullptr, *q = nullptr, *o = nullptr, *hid = nullptr, *e = nullptr, *u = nullptr;
@@ -258,6 +266,7 @@ struct tppsd_state {
   tppsd_verify_buf ivf{};
   tppsd_accept_buf iac{};
   // host-side run state
+  int n0 = 0;
   int n_gen = 0;
   int job_ctx = 0;                 // events per sequence half-way through the job of the last prefill
   int left_max = -1;               // events the slowest sequence still needs, -1: not known here
@@ -313,12 +322,28 @@ struct WsLayout {
   size_t wbT = 0, wbD = 0, wb_nT = 0, wb_nD = 0;   // matrices in the k_block order (0 bytes: not served)
   size_t d_tau, d_t, d_k, d_logg, d_logf, d_mix, d_lt, d_rate;
   size_t v_logg, v_logf, v_mix, v_lt;
+  size_t c8 = 0, k_new = 0, v_new = 0;   // TPPSD_FLAG_CACHE8
   size_t a_L, a_nnew, a_knew, a_tnew, a_taunew, a_ar, a_flags;
 };
 
+// the target's 8-bit cache: a sequence of the batch each, pages enough for all
+CacheDev cache8_geometry(const tppsd_model *T, int B, int cap) {
+  CacheDev c{};
+  c.L = T->cfg.n_layers;
+  c.H = c.KV = T->H();
+  c.dh = T->dh();
+  c.bf16 = T->bf16();
+  c.S = B;
+  c.NP = (cap + CACHE_BLOCK - 1) / CACHE_BLOCK;
+  c.n_pages = c.NP * B;
+  c.max_events = cap;
+  return c;
+}
+
 // pre_rows: rows of the activation scratch that prefill chunks use (prefill_rows, or 0 for
 // what the rounds need, which is what a workspace must hold at least)
-WsLayout ws_layout(const tppsd_model *T, const tppsd_model *D, int B, int cap, int MG, size_t pre_rows) {
+WsLayout ws_layout(const tppsd_model *T, const tppsd_model *D, int B, int cap, int MG, size_t pre_rows,
+                   unsigned flags) {
   WsLayout w;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -346,7 +371,8 @@ WsLayout ws_layout(const tppsd_model *T, const tppsd_model *D, int B, int cap, i
   w.freqT = take((size_t)T->d() * 4);
   w.freqD = take(D ? (size_t)D->d() * 4 : 0);
   const size_t kvc = kv_stride(cap);
-  w.layerT = Bz * T->H() * kvc * T->dh() * T->act_bytes();
+  const bool cache8 = (flags & TPPSD_FLAG_CACHE8) != 0;
+  w.layerT = cache8 ? 0 : Bz * T->H() * kvc * T->dh() * T->act_bytes();
   w.kT = take(w.layerT * T->cfg.n_layers);
   w.vT = take(w.layerT * T->cfg.n_layers);
   w.layerD = D ? Bz * D->H() * kvc * D->dh() * D->act_bytes() : 0;
@@ -437,6 +463,14 @@ WsLayout ws_layout(const tppsd_model *T, const tppsd_model *D, int B, int cap, i
   w.a_taunew = take(Bz * (MG + 1) * 4);
   w.a_ar = take(Bz * 4);
   w.a_flags = take(Bz);
+  if (cache8) {
+    CacheDev c = cache8_geometry(T, B, cap);
+    w.c8 = take(cache_view(&c, nullptr));
+    const size_t width = T->d() * T->act_bytes();
+    const size_t rows_new = std::max(Bz * kv_stride(Pmax), Bz * kv_stride((int)(pre_rows / Bz)));
+    w.k_new = take(rows_new * width);
+    w.v_new = take(rows_new * width);
+  }
   w.total = align_up(off);
   return w;
 }
@@ -458,6 +492,61 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
     s->ev_used[pair] = 1;
     return s->cur_ev[2 * pair + end];
   };
+  // keys and values of layer l: into the model's slab, or, for a target with an
+  // 8-bit cache, into k_new / v_new and from there into the cache
+  const bool paged = s->cache8 && m == s->T;
+  const int new_cap = kv_stride(P);
+  if (paged) {
+    CacheBegin b{};
+    b.B = B;
+    b.P = P;
+    b.start_in = start;
+    b.start_off = start_off;
+    b.done = s->done;
+    b.split_target = cache_split_target(s->c8, B, P);
+    launch_cache_begin(s->c8, b, st);
+  }
+  auto set_kv = [&](Epi &e, int l) {
+    e.kc = paged ? s->k_new : c.k + c.layer_bytes * l;
+    e.vc = paged ? s->v_new : c.v + c.layer_bytes * l;
+    e.start = paged ? s->zeros : start;
+    e.start_off = paged ? 0 : start_off;
+    e.cap = paged ? new_cap : s->kv_cap;
+  };
+  auto new_rows = [&] {
+    CacheRows r{};
+    r.k = s->k_new;
+    r.v = s->v_new;
+    r.k_sp = r.v_sp = dh;
+    r.k_sh = r.v_sh = (int64_t)new_cap * dh;
+    r.k_sb = r.v_sb = (int64_t)H * new_cap * dh;
+    r.v_blocked = bf;
+    return r;
+  };
+  // past the last layer's keys and values a pass without a decoder (prefill) uses nothing
+  auto last_kv = [&](int l) {
+    if (paged) launch_cache_append(s->c8, l, B, P, new_rows(), st);
+  };
+  auto attention = [&](int l, int sink) {
+    if (paged) {
+      CacheAttend a{};
+      a.q = s->q;
+      a.o = s->o;
+      a.ldq = a.ldo = d;
+      a.kv = new_rows();
+      a.layer = l;
+      a.B = B;
+      a.P = P;
+      a.scale = 1.f / sqrtf((float)dh);
+      a.sink = sink;
+      a.zero = 1;
+      last_kv(l);
+      launch_cache_attend(s->c8, a, st, ev(l, 0), ev(l, 1));
+      return;
+    }
+    launch_attention(s->q, c.k + c.layer_bytes * l, c.v + c.layer_bytes * l, s->o, bf, start, start_off, s->done, B,
+                     P, H, dh, s->kv_cap, s->attn_part, sink, verify, nt_keys, ev(l, 0), ev(l, 1), st);
+  };
   // LayerNorms run inside the GEMMs that consume them where the width allows
   const bool fuse_ln = gemm_ln_fusable(bf, d);
   if (m->attnhp()) {
@@ -467,25 +556,22 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
     launch_embed_attnhp(s->x, s->u, T, d, P, src, m->type_emb, bf, c.freq, m->cfg.n_types, st);
     for (int l = 0; l < L; ++l) {
       const LayerW &w = m->layers[l];
-      char *kc = c.k + c.layer_bytes * l, *vc = c.v + c.layer_bytes * l;
       Epi e{};
       e.mode = EPI_QKV;
       e.bias = w.qkv_b;
       e.q = s->q;
-      e.kc = kc;
-      e.vc = vc;
-      e.start = start;
-      e.start_off = start_off;
+      set_kv(e, l);
       e.P = P;
       e.H = H;
       e.dh = dh;
       e.d = d;
-      e.cap = s->kv_cap;
       e.status = s->status;
       launch_gemm(s->u, nullptr, w.qkv_w, bf, T, 3 * d, 2 * d, e, st, ev(L + 4 * l, 0), ev(L + 4 * l, 1));
-      if (!head && l + 1 == L) break;   // (prefill: past the last layer's keys and values nothing is used)
-      launch_attention(s->q, kc, vc, s->o, bf, start, start_off, s->done, B, P, H, dh, s->kv_cap, s->attn_part,
-                       1, verify, nt_keys, ev(l, 0), ev(l, 1), st);
+      if (!head && l + 1 == L) {
+        last_kv(l);
+        break;
+      }
+      attention(l, 1);
       launch_attnhp_update(s->x, s->o, s->u, s->a, bf, T, d, st);
     }
   }
@@ -526,15 +612,11 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
       e.mode = EPI_QKV;
       e.bias = w.qkv_b;
       e.q = s->q;
-      e.kc = c.k + c.layer_bytes * l;
-      e.vc = c.v + c.layer_bytes * l;
-      e.start = start;
-      e.start_off = start_off;
+      set_kv(e, l);
       e.P = P;
       e.H = H;
       e.dh = dh;
       e.d = d;
-      e.cap = s->kv_cap;
       e.status = s->status;
     };
     ba.first = 1;
@@ -543,11 +625,12 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
     set_qkv(0);
     launch_block(ba, bf, st, ev(L, 0), ev(L, 1));
     for (int l = 0; l < L; ++l) {
-      char *kc = c.k + c.layer_bytes * l, *vc = c.v + c.layer_bytes * l;
       const bool last = l + 1 == L;
-      if (last && !head) break;
-      launch_attention(s->q, kc, vc, s->o, bf, start, start_off, s->done, B, P, H, dh, s->kv_cap, s->attn_part,
-                       0, verify, nt_keys, ev(l, 0), ev(l, 1), st);
+      if (last && !head) {
+        last_kv(l);
+        break;
+      }
+      attention(l, 0);
       const LayerW &w = m->layers[l];
       ba.first = 0;
       ba.pre = 1;
@@ -581,15 +664,11 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
     e.mode = EPI_QKV;
     e.bias = m->layers[l].qkv_b;
     e.q = s->q;
-    e.kc = c.k + c.layer_bytes * l;
-    e.vc = c.v + c.layer_bytes * l;
-    e.start = start;
-    e.start_off = start_off;
+    set_kv(e, l);
     e.P = P;
     e.H = H;
     e.dh = dh;
     e.d = d;
-    e.cap = s->kv_cap;
     e.status = s->status;
     return e;
   };
@@ -607,7 +686,6 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
   const bool ln_gemm = fuse_ln && !gemm_ln_split(bf, d, T);
   for (int l = 0; l < m->cfg.n_layers && !m->attnhp(); ++l) {
     const LayerW &w = m->layers[l];
-    char *kc = c.k + c.layer_bytes * l, *vc = c.v + c.layer_bytes * l;
     const LnA ln1{s->x, w.ln1_g, w.ln1_b}, ln2{s->x, w.ln2_g, w.ln2_b};
     if (!(use_layer_fused && l > 0)) {   // (else the previous fused launch wrote this layer's q, k, v)
       if (!ln_gemm) launch_layernorm(s->x, s->a, bf, w.ln1_g, w.ln1_b, T, d, P, ln_tile_from, st);
@@ -615,9 +693,11 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
       launch_gemm(s->a, ln_gemm ? &ln1 : nullptr, w.qkv_w, bf, T, 3 * d, d, e, st, ev(L + 4 * l, 0),
                   ev(L + 4 * l, 1));
     }
-    if (!head && l + 1 == L) break;   // (prefill: past the last layer's keys and values nothing is used)
-    launch_attention(s->q, kc, vc, s->o, bf, start, start_off, s->done, B, P, H, dh, s->kv_cap, s->attn_part,
-                     0, verify, nt_keys, ev(l, 0), ev(l, 1), st);
+    if (!head && l + 1 == L) {
+      last_kv(l);
+      break;
+    }
+    attention(l, 0);
     if (use_layer_fused) {
       LayerArgs la{};
       la.x = s->x;
@@ -892,7 +972,7 @@ int do_draft_poisson(tppsd_state *s, int gamma, const float *params, const tppsd
 // after the pending event
 bool seq_pass_ok(const tppsd_state *s, int P) {
   const tppsd_model *m = s->T;
-  return !m->attnhp() &&
+  return !m->attnhp() && !s->cache8 &&
          verify_seq_ok(m->bf16(), m->cfg.n_layers, m->d(), m->H(), m->cfg.d_ffn, s->B, P, s->job_ctx);
 }
 
@@ -1175,33 +1255,42 @@ void tppsd_model_destroy(tppsd_model *m) { delete m; }
 
 int tppsd_state_bytes(const tppsd_model *T, const tppsd_model *D, int B, int max_events, int max_gamma,
                       size_t *bytes) {
+  return tppsd_state_bytes_flags(T, D, B, max_events, max_gamma, 0, bytes);
+}
+
+int tppsd_state_bytes_flags(const tppsd_model *T, const tppsd_model *D, int B, int max_events, int max_gamma,
+                            unsigned flags, size_t *bytes) {
   if (!T || !bytes) return fail(TPPSD_E_ARG, "null target model or output pointer");
   if (B < 1 || max_events < 3 || max_gamma < 1 || max_gamma > TPPSD_MAX_GAMMA)
     return fail(TPPSD_E_ARG, "need B >= 1, max_events >= 3, 1 <= max_gamma <= %d", TPPSD_MAX_GAMMA);
   if (D && (D->cfg.n_mix != T->cfg.n_mix || D->cfg.n_types != T->cfg.n_types))
     return fail(TPPSD_E_CONFIG, "draft and target must share n_mix and n_types");
-  *bytes = ws_layout(T, D, B, max_events, max_gamma, prefill_rows(B, max_events)).total;
+  if (flags & ~STATE_FLAGS) return fail(TPPSD_E_ARG, "unknown flags 0x%x", flags);
+  if ((flags & TPPSD_FLAG_CACHE8) && (long long)B * ((max_events + CACHE_BLOCK - 1LL) / CACHE_BLOCK) > (1 << 26))
+    return fail(TPPSD_E_ARG, "batch and max_events too large for an 8-bit cache");
+  *bytes = ws_layout(T, D, B, max_events, max_gamma, prefill_rows(B, max_events), flags).total;
   return TPPSD_OK;
 }
 
 int tppsd_state_create(const tppsd_model *T, const tppsd_model *D, int B, int max_events, int max_gamma,
                        uint64_t seed, unsigned flags, void *d_ws, size_t ws_bytes, tppsd_state **out) {
   size_t need = 0;
-  if (int rc = tppsd_state_bytes(T, D, B, max_events, max_gamma, &need)) return rc;
+  if (int rc = tppsd_state_bytes_flags(T, D, B, max_events, max_gamma, flags & STATE_FLAGS, &need)) return rc;
   if (!d_ws || !out) return fail(TPPSD_E_ARG, "null workspace or output pointer");
   if ((uintptr_t)d_ws % ALIGN) return fail(TPPSD_E_WORKSPACE, "workspace must be 256-byte aligned");
   // a smaller workspace that holds the rounds' scratch is taken too: prefill then runs in
   // the longest chunks of whole PREFILL_CHUNKs that it has the rows for
   size_t pre_rows = prefill_rows(B, max_events);
   if (ws_bytes < need) {
-    if (ws_bytes < ws_layout(T, D, B, max_events, max_gamma, 0).total)
+    if (ws_bytes < ws_layout(T, D, B, max_events, max_gamma, 0, flags).total)
       return fail(TPPSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
     size_t most = pre_rows / B / PREFILL_CHUNK;
-    while (most > 0 && ws_bytes < ws_layout(T, D, B, max_events, max_gamma, B * most * PREFILL_CHUNK).total) --most;
+    while (most > 0 && ws_bytes < ws_layout(T, D, B, max_events, max_gamma, B * most * PREFILL_CHUNK, flags).total)
+      --most;
     pre_rows = B * most * PREFILL_CHUNK;
   }
-  if (flags & ~TPPSD_FLAG_BONUS) return fail(TPPSD_E_ARG, "unknown flags 0x%x", flags);
-  const WsLayout w = ws_layout(T, D, B, max_events, max_gamma, pre_rows);
+  if (flags & ~STATE_FLAGS) return fail(TPPSD_E_ARG, "unknown flags 0x%x", flags);
+  const WsLayout w = ws_layout(T, D, B, max_events, max_gamma, pre_rows, flags);
   tppsd_state *s = new tppsd_state();
   s->T = T;
   s->D = D;
@@ -1233,6 +1322,14 @@ int tppsd_state_create(const tppsd_model *T, const tppsd_model *D, int B, int ma
   s->cT.v = ws + w.vT;
   s->cT.layer_bytes = w.layerT;
   s->cT.freq = (float *)(ws + w.freqT);
+  s->cache8 = (flags & TPPSD_FLAG_CACHE8) != 0;
+  if (s->cache8) {
+    s->c8 = cache8_geometry(T, B, max_events);
+    cache_view(&s->c8, ws + w.c8);
+    s->c8.status = s->status;
+    s->k_new = ws + w.k_new;
+    s->v_new = ws + w.v_new;
+  }
   if (D) {
     s->cD.k = ws + w.kD;
     s->cD.v = ws + w.vD;
@@ -1386,21 +1483,11 @@ void tppsd_state_destroy(tppsd_state *s) {
   delete s;
 }
 
-int tppsd_prefill(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, int n_gen, hipStream_t st) {
-  return tppsd_prefill_window(s, d_t, d_k, n0, n_gen, nullptr, st);
-}
+}  // extern "C"
 
-int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, int n_gen,
-                         const float *d_t_end, hipStream_t st) {
-  if (!s || !d_t || !d_k) return fail(TPPSD_E_ARG, "null argument");
-  if (n0 < 2 || n_gen < 0) return fail(TPPSD_E_ARG, "need n0 >= 2 and n_gen >= 0");
-  if ((long long)n0 + n_gen + s->max_gamma + 1 > s->cap)
-    return fail(TPPSD_E_ARG, "n0 + n_gen + max_gamma + 1 = %lld exceeds max_events %d",
-                (long long)n0 + n_gen + s->max_gamma + 1, s->cap);
-  s->n_gen = n_gen;
-  s->windowed = d_t_end != nullptr;
-  s->left_max = s->windowed ? -1 : n_gen;
-  s->job_ctx = n0 + n_gen / 2;
+namespace {
+// the models' weights in the forms and orders that the kernels read, once per state
+void build_forms(tppsd_state *s, hipStream_t st) {
   if (!s->heads_built) {
     for (int which = 0; which < (s->D ? 2 : 1); ++which) {
       const tppsd_model *m = which ? s->D : s->T;
@@ -1462,6 +1549,29 @@ int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, i
     }
     s->packs_built = true;
   }
+}
+}  // namespace
+
+extern "C" {
+
+int tppsd_prefill(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, int n_gen, hipStream_t st) {
+  return tppsd_prefill_window(s, d_t, d_k, n0, n_gen, nullptr, st);
+}
+
+int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, int n0, int n_gen,
+                         const float *d_t_end, hipStream_t st) {
+  if (!s || !d_t || !d_k) return fail(TPPSD_E_ARG, "null argument");
+  if (n0 < 2 || n_gen < 0) return fail(TPPSD_E_ARG, "need n0 >= 2 and n_gen >= 0");
+  if ((long long)n0 + n_gen + s->max_gamma + 1 > s->cap)
+    return fail(TPPSD_E_ARG, "n0 + n_gen + max_gamma + 1 = %lld exceeds max_events %d",
+                (long long)n0 + n_gen + s->max_gamma + 1, s->cap);
+  s->n0 = n0;
+  s->n_gen = n_gen;
+  s->windowed = d_t_end != nullptr;
+  s->left_max = s->windowed ? -1 : n_gen;
+  s->job_ctx = n0 + n_gen / 2;
+  build_forms(s, st);
+  if (s->cache8) launch_cache_reset(s->c8, st);
   launch_prefill_init(d_t, d_k, s->B, n0, n_gen, d_t_end, s->ev_t, s->ev_k, s->cap, s->n, s->gen, s->lenT, s->lenD,
                       s->done, s->rnd, s->zeros, s->t_end, s->ll, s->n_done, s->status, s->acc_stats, st);
   // encode history events 0 .. n0 - 2 (target) and 0 .. n0 - 3 (draft) in position chunks
@@ -1485,6 +1595,51 @@ int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, i
   s->draft_ok = s->D != nullptr;
   s->drafted_this_round = false;
   return hip_check("tppsd_prefill");
+}
+
+int tppsd_state_fork(tppsd_state *to, tppsd_state *from, const int32_t *d_parent, hipStream_t st) {
+  if (!to || !from || !d_parent) return fail(TPPSD_E_ARG, "null argument");
+  if (to->T != from->T || to->D != from->D) return fail(TPPSD_E_CONFIG, "states of different models");
+  if (to->cache8 != from->cache8) return fail(TPPSD_E_CONFIG, "one of the states has an 8-bit cache");
+  if (!from->prefilled) return fail(TPPSD_E_ORDER, "call tppsd_prefill first");
+  if ((long long)from->n0 + from->n_gen + to->max_gamma + 1 > to->cap)
+    return fail(TPPSD_E_ARG, "n0 + n_gen + max_gamma + 1 = %lld exceeds max_events %d",
+                (long long)from->n0 + from->n_gen + to->max_gamma + 1, to->cap);
+  const bool same = to == from;
+  build_forms(to, st);
+  auto side = [](tppsd_state *s) {
+    return ForkSide{s->B, s->cap, s->ev_t, s->ev_k, s->n, s->gen, s->lenT, s->lenD, s->done, s->rnd, s->zeros,
+                    s->t_end, s->ll, s->n_done, s->status, s->acc_stats};
+  };
+  const ForkSide a = side(from), b = side(to);
+  // (the round buffers hold nothing between rounds)
+  int32_t *const src = to->iac.L, *const dst = to->iac.n_new;
+  if (to->cache8 && !same) launch_cache_reset(to->c8, st);
+  launch_fork_pairs(b, a, d_parent, same, src, dst, st);
+  if (to->cache8) {
+    // the cache learns lengths from the passes: those of the last accept
+    launch_snapshot(from->lenT, from->c8.lens, from->B, st);
+    if (same) launch_cache_fork(to->c8, to->B, src, dst, st);
+    else launch_cache_copy(to->c8, from->c8, to->B, src, dst, st);
+  }
+  for (int which = 0; which < (to->D ? 2 : 1); ++which) {
+    const tppsd_model *m = which ? to->D : to->T;
+    const ModelCache &cb = which ? to->cD : to->cT, &ca = which ? from->cD : from->cT;
+    if (!cb.layer_bytes) continue;
+    launch_fork_slabs(ForkSlab{cb.k, cb.v, cb.layer_bytes, to->kv_cap}, ForkSlab{ca.k, ca.v, ca.layer_bytes, from->kv_cap},
+                      to->B, m->cfg.n_layers, m->H(), m->dh(), (int)m->act_bytes(), src, dst,
+                      which ? from->lenD : from->lenT, st);
+  }
+  launch_fork_state(b, a, same, src, dst, st);
+  to->n0 = from->n0;
+  to->n_gen = from->n_gen;
+  to->windowed = from->windowed;
+  to->job_ctx = from->job_ctx;
+  to->left_max = -1;
+  to->prefilled = true;
+  to->draft_ok = from->draft_ok;
+  to->drafted_this_round = false;
+  return hip_check("tppsd_state_fork");
 }
 
 static int check_round(tppsd_state *s, int gamma) {

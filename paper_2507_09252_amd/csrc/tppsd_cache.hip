@@ -239,7 +239,8 @@ __global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t 
 
 // Which pairs of a fork or copy are carried out: both sequences exist, a
 // destination is named once (the first pair counts) and, within one cache, is
-// no pair's source. Verdicts into to.p_seq.
+// no pair's source. A pair of two negative numbers is none. Verdicts into
+// to.p_seq.
 __global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev from, int n, const int32_t *src,
                                                          const int32_t *dst, int same) {
   auto ok = [&](int i) { return src[i] >= 0 && src[i] < from.S && dst[i] >= 0 && dst[i] < to.S; };
@@ -264,7 +265,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev f
   for (int i = threadIdx.x; i < n; i += PLAN_NT) {
     bool good = ok(i) && ld_agent(&to.owner[dst[i]]) == i;
     if (good && same) good = !ld_agent(&to.role[dst[i]]);
-    if (!good) atomicOr(to.status, TPPSD_STATUS_SEQUENCE);
+    if (!good && (src[i] >= 0 || dst[i] >= 0)) atomicOr(to.status, TPPSD_STATUS_SEQUENCE);
     if (good && from.lens[src[i]] > to.max_events) {
       atomicOr(to.status, TPPSD_STATUS_CAPACITY);
       good = false;
@@ -491,7 +492,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int
   // the first block's slots may be those of a block that the ring keeps: that
   // block's rows go in here, behind the reads of the old ones
   const int later = (last - first) % 2 == 0 ? last : last - 1;
-  const bool shares = later > first && old > 0;
+  const bool shares = later > first && start % CACHE_BLOCK != 0;
   if (blk == first && P > CACHE_BLOCK && old > 0) {   // the attention of this call still needs the old rows
     ACT *st = (ACT *)c.stash + ((size_t)i * c.KV + h) * 2 * CACHE_BLOCK * DH;
     for (int x = tid; x < old * DH; x += 256) {

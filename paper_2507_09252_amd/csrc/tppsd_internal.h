@@ -88,6 +88,11 @@ struct HeadArgs {
   const int32_t *gen0;
 };
 
+// A fork within a state moves the continued sequence's round counter past every
+// round that it or its source has drawn for: its bits from FORK_SHIFT up count
+// forks, and are the third counter word of AR draws (0 without forks).
+constexpr int FORK_SHIFT = 20;
+
 struct AcceptArgs {
   int B, gamma, M, K, max_gamma, bonus;
   const float *d_tau, *d_t, *d_logg, *d_logf, *d_mix, *d_logtype;
@@ -288,6 +293,34 @@ struct PoissonDraftArgs {
 };
 void launch_poisson_fit(const float *t, const int32_t *k, int B, int n0, int K, float *params, hipStream_t st);
 void launch_draft_poisson(const PoissonDraftArgs &a, hipStream_t st);
+
+// Continuing sequences of one state in another, or in itself (tppsd_fork.hip):
+// sequence b of `to` takes everything of sequence parent[b] of `from`
+struct ForkSide {
+  int B, cap;
+  float *ev_t;
+  int32_t *ev_k;
+  int32_t *n, *gen, *lenT, *lenD, *done, *rnd, *zeros;
+  float *t_end;
+  double *ll;
+  int32_t *n_done;
+  uint32_t *status;
+  unsigned long long *acc_stats;
+};
+// slabs of a contiguous cache: [L][B][H][kv_cap][dh], `elt` bytes an element
+struct ForkSlab {
+  char *k, *v;
+  size_t layer_bytes;
+  int kv_cap;
+};
+// verdicts (1: carried out) into ok[to.B]; sources into src, destinations into
+// dst with -1 where a sequence stays as it is
+void launch_fork_pairs(const ForkSide &to, const ForkSide &from, const int32_t *parent, int same, int32_t *src,
+                       int32_t *dst, hipStream_t st);
+void launch_fork_slabs(const ForkSlab &to, const ForkSlab &from, int B, int L, int H, int dh, int elt,
+                       const int32_t *src, const int32_t *dst, const int32_t *len, hipStream_t st);
+void launch_fork_state(const ForkSide &to, const ForkSide &from, int same, const int32_t *src, const int32_t *dst,
+                       hipStream_t st);
 
 // ---- launchers (tppsd_kernels.hip) ----
 void launch_draft_fused(const DraftArgs &a, int bf16, hipStream_t st, hipEvent_t ev0 = nullptr,

@@ -1769,7 +1769,7 @@ __device__ void head_row(const float *lr, int M, int K, const HeadArgs &a, int b
     if (!active) return;
     float u[4];
     const int g = a.gen[b];
-    philox_uniforms(a.seed, (uint64_t)b, (uint64_t)g, 0ull, TAG_AR, u);
+    philox_uniforms(a.seed, (uint64_t)b, (uint64_t)g, (uint64_t)((uint32_t)a.rnd[b] >> FORK_SHIFT), TAG_AR, u);
     const float tau = draw_tau(u);
     const int kk = sample(logk, K, u[3]);
     const int n = a.n[b];

@@ -20,7 +20,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libtppsd.so
 
 TPPSD_OK = 0
 PREC = {"fp32": 0, "bf16": 1}
-FLAG_BONUS = 1
+FLAG_BONUS, FLAG_CACHE8 = 1, 2
 STATUS_CAPACITY, STATUS_NONFINITE, STATUS_AR_CAP = 1, 2, 4
 STATUS_PAGES, STATUS_SEQUENCE, STATUS_OPEN = 8, 16, 32
 CACHE_BLOCK, CACHE_RING = 64, 128
@@ -38,6 +38,7 @@ EXPORTS = [
     "tppsd_cache_bytes", "tppsd_cache_entry", "tppsd_cache_create", "tppsd_cache_destroy", "tppsd_cache_reset",
     "tppsd_cache_begin", "tppsd_cache_append", "tppsd_cache_attend", "tppsd_cache_commit", "tppsd_cache_truncate",
     "tppsd_cache_fork", "tppsd_cache_copy", "tppsd_cache_read", "tppsd_cache_status",
+    "tppsd_state_bytes_flags", "tppsd_state_fork",
 ]
 
 
@@ -128,6 +129,8 @@ def lib():
         "tppsd_sample_sd_poisson": (c_int, [c_void_p, c_int, c_void_p, c_int, P(c_int), c_void_p]),
         "tppsd_prefill_window": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_int, c_void_p, c_void_p]),
         "tppsd_read_loglik": (c_int, [c_void_p, c_void_p, c_void_p]),
+        "tppsd_state_bytes_flags": (c_int, [c_void_p, c_void_p, c_int, c_int, c_int, c_uint, P(c_size_t)]),
+        "tppsd_state_fork": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p]),
         "tppsd_cache_bytes": (c_int, [P(CacheCfgC), P(c_size_t)]),
         "tppsd_cache_entry": (c_int, [P(CacheCfgC), c_int, P(c_char_p), P(c_size_t)]),
         "tppsd_cache_create": (c_int, [P(CacheCfgC), c_void_p, c_size_t, P(c_void_p)]),
@@ -295,19 +298,21 @@ class AcceptBuffers:
 # ---------------------------------------------------------------------------
 
 class State:
-    """tppsd_state over a torch-allocated workspace; methods map 1:1 to the C ABI."""
+    """tppsd_state over a torch-allocated workspace; methods map 1:1 to the C ABI.
+    cache8: the target's keys and values in an 8-bit paged cache (TPPSD_FLAG_CACHE8)."""
 
     def __init__(self, target: Model, draft: Optional[Model], B: int, max_events: int, max_gamma: int,
-                 seed: int = 0, bonus: bool = True, device="cuda"):
+                 seed: int = 0, bonus: bool = True, device="cuda", cache8: bool = False):
         self.target, self.draft = target, draft
         self.B, self.max_events, self.max_gamma = B, max_events, max_gamma
         n = c_size_t()
         dh = draft.handle if draft is not None else None
-        _check(lib().tppsd_state_bytes(target.handle, dh, B, max_events, max_gamma, ctypes.byref(n)))
+        flags = (FLAG_BONUS if bonus else 0) | (FLAG_CACHE8 if cache8 else 0)
+        _check(lib().tppsd_state_bytes_flags(target.handle, dh, B, max_events, max_gamma, flags, ctypes.byref(n)))
         self.ws = torch.empty(n.value, dtype=torch.uint8, device=device)
         h = c_void_p()
         _check(lib().tppsd_state_create(target.handle, dh, B, max_events, max_gamma, c_uint64(seed),
-                                        FLAG_BONUS if bonus else 0, _ptr(self.ws), n.value, ctypes.byref(h)))
+                                        flags, _ptr(self.ws), n.value, ctypes.byref(h)))
         self.handle = h
 
     def __del__(self):
@@ -327,6 +332,14 @@ class State:
             self._t_end = t_end
             _check(lib().tppsd_prefill_window(self.handle, _ptr(t), _ptr(k), t.shape[1], n_gen, _ptr(t_end),
                                               _stream()))
+
+    def tppsd_state_fork(self, source: "State", parent: torch.Tensor):
+        """Sequence b becomes a copy of source's sequence parent[b] (source may be self)."""
+        parent = parent.to(torch.int32).contiguous()
+        if parent.numel() != self.B or parent.device != self.ws.device:
+            raise TppsdError(1, f"parent must hold {self.B} sequences on {self.ws.device}")
+        self._parent = parent
+        _check(lib().tppsd_state_fork(self.handle, source.handle, _ptr(parent), _stream()))
 
     def tppsd_draft(self, gamma: int, out: DraftBuffers):
         _check(lib().tppsd_draft(self.handle, gamma, ctypes.byref(out.c()), _stream()))
