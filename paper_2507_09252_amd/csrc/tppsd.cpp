@@ -540,7 +540,6 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
       a.scale = 1.f / sqrtf((float)dh);
       a.sink = sink;
       a.zero = 1;
-      last_kv(l);
       launch_cache_attend(s->c8, a, st, ev(l, 0), ev(l, 1));
       return;
     }

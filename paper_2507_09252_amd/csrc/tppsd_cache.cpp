@@ -90,6 +90,7 @@ size_t view(CacheDev *c, char *ws, Entry *entries) {
   c->max_items = cache_max_items(c->S, c->KV);
   take(c->items, (size_t)c->max_items * 16);
   take(c->part, cache_part_floats(*c) * 4);
+  take(c->joins, CACHE_JOINS * 4);
   take(c->stash, S * KV * 2 * CACHE_BLOCK * dh * e);
   take(c->status, 4);
   return (off + ALIGN - 1) / ALIGN * ALIGN;
@@ -235,7 +236,6 @@ int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
   a.P = c->P;
   a.scale = scale;
   a.sink = sink != 0;
-  launch_cache_append(c->d, layer, c->B, c->P, a.kv, st);
   launch_cache_attend(c->d, a, st);
   return hip_check("tppsd_cache_attend");
 }

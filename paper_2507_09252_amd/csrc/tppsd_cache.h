@@ -20,8 +20,10 @@ constexpr int CACHE_RING = 128;   // tail rows: two blocks
 // Least exponent of a scale: 2^-100 keeps every code's value, and its product
 // with the reciprocal scale, a normal fp32 (and bf16) number
 constexpr int CACHE_E_MIN = -100;
-// workgroups that the split attention aims at (two per CU and some)
-constexpr int CACHE_SPLIT_WGS = 1024;
+// Workgroups of the attention that make a full chip (one per CU), the fewest
+// pages of a piece of a row, and the most (row, head, group) triples of a batch
+// whose rows are split
+constexpr int CACHE_SPLIT_WGS = 256, CACHE_MIN_PIECE = 8, CACHE_JOINS = 4096;
 
 struct CacheDev {
   int L, H, KV, dh, bf16;
@@ -44,10 +46,11 @@ struct CacheDev {
   int32_t *counts;    // [8] scratch: items of the plan, pages to copy
   // plan of the call in progress, one row per sequence of the batch
   int32_t *p_seq, *p_start, *p_count;   // [S]
-  int32_t *p_item;    // [S + 1] first item of each row (split attention)
-  int4 *items;        // work items: row, first page, end page, last of its row
+  int32_t *p_item;    // [S + 1] first item of each row
+  int4 *items;        // work items: row, first page, end page, slot of the partial state (-1: the row's one item)
   int max_items;
-  float *part;        // split partials
+  float *part;        // partial states of split rows
+  int32_t *joins;     // [CACHE_JOINS] splits that have arrived; zero between calls
   char *stash;        // [S][KV][2][64][dh] rows of a long chunk's first block from before it
   uint32_t *status;
 };
@@ -68,7 +71,7 @@ struct CacheBegin {
   int B, P;
   const int32_t *seqs, *counts, *start_in, *done;
   int start_off;
-  int split_target;   // items of the split attention over the batch, 0: one per row
+  int split_target;   // full chip: items of the batch, 0: one per row
 };
 
 struct CacheAttend {
@@ -84,6 +87,7 @@ struct CacheAttend {
 
 void launch_cache_reset(const CacheDev &c, hipStream_t st);
 void launch_cache_begin(const CacheDev &c, const CacheBegin &b, hipStream_t st);
+// (launch_cache_attend appends as well)
 void launch_cache_append(const CacheDev &c, int layer, int B, int P, const CacheRows &r, hipStream_t st);
 void launch_cache_commit(const CacheDev &c, int B, const int32_t *accept, hipStream_t st);
 void launch_cache_truncate(const CacheDev &c, int n, const int32_t *seqs, const int32_t *lens, hipStream_t st);
@@ -93,8 +97,8 @@ void launch_cache_copy(const CacheDev &to, const CacheDev &from, int n, const in
 void launch_cache_read(const CacheDev &c, int layer, int n, const int32_t *seqs, const int32_t *first, int count,
                        void *k, void *v, hipStream_t st);
 
-// split attention for a batch of B rows of P positions: items over the batch,
-// 0 where one workgroup per (row, head, group of query rows) is taken
+// items that make a full chip for a batch of B rows of P positions, 0 where
+// rows are not split
 int cache_split_target(const CacheDev &c, int B, int P);
 int cache_max_items(int S, int KV);
 size_t cache_part_floats(const CacheDev &c);

@@ -7,8 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/tppsd.h"
-#include "tppsd_cache.h"
-#include "tppsd_device.h"
+#include "tppsd_cache_device.h"
 
 namespace tppsd {
 
@@ -86,6 +85,7 @@ __global__ void k_cache_reset(CacheDev c) {
     c.freeb[j] = left >= 32 ? 0xFFFFFFFFu : (1u << left) - 1u;
     c.mark[j] = 0u;
   }
+  for (size_t j = i; j < (size_t)CACHE_JOINS; j += n) c.joins[j] = 0;
   if (i == 0) *c.status = 0u;
 }
 
@@ -94,7 +94,8 @@ __global__ void k_cache_reset(CacheDev c) {
 // the work items of the split attention. One workgroup: the whole batch's
 // bookkeeping is a few thousand integers.
 __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
-  const int tid = threadIdx.x;
+  __shared__ int tops[PLAN_NT / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (b.B + PLAN_NT - 1) / PLAN_NT, i0 = min(b.B, tid * per), i1 = min(b.B, i0 + per);
   if (b.seqs) {
     // a sequence that is named twice belongs to the first row that names it
@@ -136,7 +137,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
   int total;
   int off = block_scan(need_sum, &total);
   const int avail = total > 0 ? list_bits(c.freeb, c.n_pages, total, c.list) : 0;
-  int pages_sum = 0;
+  int pages_sum = 0, top_max = 0;
   for (int i = i0; i < i1; ++i) {
     const int s = c.p_seq[i];
     if (s < 0) continue;
@@ -163,27 +164,44 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
       const int top = (start + cnt - 1) / CACHE_BLOCK;
       c.low[s] = max(top - 1, min(c.low[s], start / CACHE_BLOCK));
       pages_sum += top;
+      top_max = max(top_max, top);
     }
   }
-  // work items: equal page ranges over the batch, about split_target of them
+  // Work items. Rows of about equal length that fill the chip are taken whole;
+  // otherwise pages are dealt out in pieces of a third of a workgroup's share.
+  // Pieces of the same row share one of the slots that their partial states take.
   int all_pages;
   block_scan(pages_sum, &all_pages);
-  const int chunk = b.split_target > 0 ? max(4, (all_pages + b.split_target - 1) / b.split_target) : INT32_MAX;
-  int item_sum = 0;
+  if (lane == 0) tops[wave] = 0;
+  __syncthreads();
+  const int wave_top = (int)lanes_max((float)top_max);
+  if (lane == 0) tops[wave] = wave_top;
+  __syncthreads();
+  int most = 0;
+#pragma unroll
+  for (int w = 0; w < PLAN_NT / 64; ++w) most = max(most, tops[w]);
+  int chunk = INT32_MAX;
+  if (b.split_target > 0) {
+    const int share = (all_pages + b.split_target - 1) / b.split_target;
+    if (most > share + share / 4) chunk = max(CACHE_MIN_PIECE, (all_pages + 3 * b.split_target - 1) / (3 * b.split_target));
+  }
   auto splits = [&](int i) {
     const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0;
-    return chunk == INT32_MAX || top <= chunk ? 1 : (top + chunk - 1) / chunk;
+    return top <= chunk ? 1 : (top + chunk - 1) / chunk;
   };
-  for (int i = i0; i < i1; ++i) item_sum += splits(i);
-  int n_items;
-  int at = block_scan(item_sum, &n_items);
+  int item_sum = 0, slot_sum = 0;
+  for (int i = i0; i < i1; ++i) {
+    const int n = splits(i);
+    item_sum += n;
+    slot_sum += n > 1 ? n : 0;
+  }
+  int n_items, n_slots;
+  int at = block_scan(item_sum, &n_items), slot = block_scan(slot_sum, &n_slots);
   for (int i = i0; i < i1; ++i) {
     const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0, n = splits(i);
     c.p_item[i] = at;
-    for (int j = 0; j < n; ++j) {
-      const int lo = n == 1 ? 0 : j * chunk, hi = n == 1 ? top : min(top, lo + chunk);
-      c.items[at++] = make_int4(i, lo, hi, j + 1 == n);
-    }
+    for (int j = 0; j < n; ++j)
+      c.items[at++] = n == 1 ? make_int4(i, 0, top, -1) : make_int4(i, j * chunk, min(top, (j + 1) * chunk), slot++);
   }
   if (tid == 0) {
     c.p_item[b.B] = n_items;
@@ -388,64 +406,9 @@ __global__ void k_copy_data(CacheDev to, CacheDev from, int n, const int32_t *sr
   }
 }
 
-// ---- fragment order ---------------------------------------------------------
-// A (page, layer, head) tile is the keys' 64 dh codes, then the values'. The
-// attention reads both in 16-byte words, word c of lane l = 16 g + m at
-// c 1024 + 16 l:
-//   keys: fragment (tile t of 16 keys, k step s) holds key 16 t + m, columns
-//     32 s + 8 g .. + 7 (d_head 16: columns 4 g .. + 3 of the one step)
-//   values: fragment (column tile u, half w) holds column 16 u + m of the keys
-//     16 (2 w + (j >> 2)) + 4 g + (j & 3), j = 0..7: the keys whose scores that
-//     lane group holds after the S^T products of tiles 2 w and 2 w + 1
-// byte i of word c of lane l of the keys: (key, column)
-template <int DH> __device__ __forceinline__ void key_at(int c, int lane, int i, int &key, int &col) {
-  const int m = lane & 15, g = lane >> 4;
-  if (DH == 16) {
-    key = 16 * (i >> 2) + m;
-    col = 4 * g + (i & 3);
-  } else {
-    constexpr int NS = DH >= 32 ? DH / 32 : 1;
-    const int f = 2 * c + (i >> 3), t = f / NS, s = f - t * NS;
-    key = 16 * t + m;
-    col = 32 * s + 8 * g + (i & 7);
-  }
-}
-__device__ __forceinline__ void value_at(int c, int lane, int i, int &key, int &col) {
-  const int m = lane & 15, g = lane >> 4, w = i >> 3, j = i & 7;
-  key = 16 * (2 * w + (j >> 2)) + 4 * g + (j & 3);
-  col = 16 * c + m;
-}
-// where element (key, column) is
-template <int DH> __device__ __forceinline__ int key_byte(int key, int col) {
-  const int t = key >> 4, m = key & 15;
-  if (DH == 16) return (16 * (col >> 2) + m) * 16 + t * 4 + (col & 3);
-  constexpr int NS = DH >= 32 ? DH / 32 : 1;
-  const int f = t * NS + (col >> 5), g = (col >> 3) & 3;
-  return (f >> 1) * 1024 + (16 * g + m) * 16 + (f & 1) * 8 + (col & 7);
-}
-__device__ __forceinline__ int value_byte(int key, int col) {
-  const int t = key >> 4, g = (key >> 2) & 3;
-  return (col >> 4) * 1024 + (16 * g + (col & 15)) * 16 + (t >> 1) * 8 + (t & 1) * 4 + (key & 3);
-}
-
 template <typename ACT> __device__ __forceinline__ size_t v_off(const CacheRows &r, int i, int p, int h, int dh, int j) {
   return r.v_blocked ? i * r.v_sb + h * r.v_sh + (size_t)(p >> 3) * 8 * dh + j * 8 + (p & 7)
                      : i * r.v_sb + p * r.v_sp + h * r.v_sh + j;
-}
-
-// exponent of the scale for block maximum m (>= 0, finite): the least e with m <= 448 2^e
-__device__ __forceinline__ int scale_exp(float m) {
-  const uint32_t u = __float_as_uint(m);
-  if (m == 0.f) return 0;
-  // 448 = 1.75 2^8 (subnormal maxima fall under the least exponent anyway)
-  const int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  return max(e, CACHE_E_MIN);
-}
-
-// x 2^-e as an e4m3 code; infinities and NaN become NaN
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float inv) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
 }
 
 // Appends to one layer. Grid (row, key/value head, block of positions that the

@@ -22,8 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "tppsd_cache.h"
-#include "tppsd_device.h"
+#include "tppsd_cache_device.h"
 
 namespace tppsd {
 
@@ -34,12 +33,6 @@ constexpr float LOG2E = 1.4426950408889634f;
 // 8 values as bf16 operands: one part for bf16 sources; for fp32 three parts
 // that add up to the value (each the bf16 rounding of what the ones before
 // leave)
-template <int NP> struct Parts {
-  bf16x8_t p[NP];
-};
-template <int NP> struct Parts4 {
-  short4_t p[NP];
-};
 // nearest bf16 pairs of 8 values, and what they leave (kept in x)
 __device__ __forceinline__ uint4 take8(float (&x)[8], bool rest) {
   uint32_t w[4];
@@ -77,10 +70,88 @@ __device__ __forceinline__ f32x4_t mma(short4_t a, short4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
 
-// NP: bf16 parts of a query or probability (1 for bf16 models, 3 for fp32);
-// MT: query tiles of 16 per wave; WK: 4 = the workgroup's waves share the
-// queries and split the keys, 1 = each wave has its own queries
-template <typename ACT, int DH, int MT, int WK> struct Attend {
+// 8 elements between memory (16-byte aligned) and registers
+template <typename ACT> __device__ __forceinline__ void load8(ACT (&x)[8], const ACT *p) {
+  constexpr int W = sizeof(ACT) * 8 / 16;
+  uint4 w[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = ((const uint4 *)p)[i];
+  __builtin_memcpy(x, w, sizeof x);
+}
+template <typename ACT> __device__ __forceinline__ void store8(ACT *p, const ACT (&x)[8]) {
+  constexpr int W = sizeof(ACT) * 8 / 16;
+  uint4 w[W];
+  __builtin_memcpy(w, x, sizeof x);
+#pragma unroll
+  for (int i = 0; i < W; ++i) ((uint4 *)p)[i] = w[i];
+}
+
+// the operand of a query or key row at p (8 elements, 4 for d_head 16), part by part into to(part)
+template <typename ACT, int DH, typename TO> __device__ __forceinline__ void load_k(const ACT *p, TO to) {
+  if constexpr (sizeof(ACT) == 2) {
+    to(0) = *(const std::remove_reference_t<decltype(to(0))> *)p;
+  } else {
+    float x[8] = {};
+    const f32x4_t a = *(const f32x4_t *)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i];
+    if constexpr (DH >= 32) {
+      const f32x4_t b = *(const f32x4_t *)(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 + i] = b[i];
+    }
+#pragma unroll
+    for (int n = 0; n < 3; ++n) {
+      const uint4 w = take8(x, n < 2);
+      if constexpr (DH >= 32) to(n) = __builtin_bit_cast(bf16x8_t, w);
+      else to(n) = __builtin_bit_cast(short4_t, make_uint2(w.x, w.y));
+    }
+  }
+}
+
+// halves of w that are not finite bf16, as 0xFFFF
+__device__ __forceinline__ uint32_t bf_bad(uint32_t w) {
+  return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
+
+// The operand of 8 values of a column, four at p and four at p + 16, in parts;
+// clean: those that are not finite as 0, or (bad) 1 in their place and 0 elsewhere.
+template <int NP> __device__ __forceinline__ void value8(const bf16_t *p, bool clean, bf16x8_t (&v)[NP]) {
+  const uint2 a = *(const uint2 *)p, b = *(const uint2 *)(p + 16);
+  uint4 w = make_uint4(a.x, a.y, b.x, b.y);
+  if (clean) w = make_uint4(w.x & ~bf_bad(w.x), w.y & ~bf_bad(w.y), w.z & ~bf_bad(w.z), w.w & ~bf_bad(w.w));
+  v[0] = __builtin_bit_cast(bf16x8_t, w);
+}
+template <int NP> __device__ __forceinline__ void value8(const float *p, bool clean, bf16x8_t (&v)[NP]) {
+  const f32x4_t a = *(const f32x4_t *)p, b = *(const f32x4_t *)(p + 16);
+  float x[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
+  if (clean)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = not_finite(x[i]) ? 0.f : x[i];
+  split8<NP>(x, v);
+}
+__device__ __forceinline__ bf16x8_t bad8(const bf16_t *p) {
+  const uint2 a = *(const uint2 *)p, b = *(const uint2 *)(p + 16);
+  const uint32_t one = 0x3F803F80u;
+  return __builtin_bit_cast(bf16x8_t, make_uint4(bf_bad(a.x) & one, bf_bad(a.y) & one, bf_bad(b.x) & one, bf_bad(b.y) & one));
+}
+__device__ __forceinline__ bf16x8_t bad8(const float *p) {
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float *q = p + (i >> 1) * 16 + (i & 1) * 2;
+    y[i] = (not_finite(q[0]) ? 0x3F80u : 0u) | (not_finite(q[1]) ? 0x3F800000u : 0u);
+  }
+  return __builtin_bit_cast(bf16x8_t, make_uint4(y[0], y[1], y[2], y[3]));
+}
+
+// What a wave holds of its query rows: operands, running maxima, sums and
+// outputs. NP: bf16 parts of a query or probability (1 for bf16 models, 3 for
+// fp32); MT: tiles of 16 query rows.
+template <typename ACT, int DH, int MT> struct Rows {
   static constexpr int NP = sizeof(ACT) == 2 ? 1 : 3;
   static constexpr int NS = DH >= 32 ? DH / 32 : 1;   // k steps of a score
   static constexpr int NU = DH / 16;                  // column tiles; also 16-byte words of a lane per side
@@ -89,23 +160,22 @@ template <typename ACT, int DH, int MT, int WK> struct Attend {
   kfrag q[MT][NP][NS];
   f32x4_t o[MT][NU];
   f32x4_t l1[MT];     // bf16: sums of the rounded probabilities (rows of ones through the matrix unit)
-  float l[MT], m[MT];
+  float l[MT], m[MT]; // fp32: this lane's keys' sum; running maximum, in base-2 units
   int pos[MT];        // position of this lane's query
-  float scale2;
-  int rr, g;
+  float scale2;       // scale log2 e: exponentials are one exp2 each
+  int g;
 
-  // One tile of 64 keys: kf(t, s, part) and vf(u, w, part) give the operands,
-  // seen(t, key) whether this lane's query of tile t sees key; KP: parts of a key
-  // or value (1: page codes or bf16 rows)
-  template <int KP, bool MASK, typename KF, typename VF, typename SEEN>
-  __device__ __forceinline__ void tile(KF kf, VF vf, SEEN seen, bool poison) {
+  // Scores and probabilities of 64 keys: kf(tile, k step, part) gives the key
+  // operand of KP parts, seen(t, key) whether this lane's query of tile t sees it.
+  template <int KP, bool MASK, typename KF, typename SEEN>
+  __device__ __forceinline__ void scores(KF kf, SEEN seen, bf16x8_t (&p)[MT][NP][2]) {
     f32x4_t s[MT][4];
 #pragma unroll
     for (int t4 = 0; t4 < 4; ++t4) {
 #pragma unroll
       for (int t = 0; t < MT; ++t) s[t][t4] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < NS; ++ks) {
+      for (int ks = 0; ks < NS; ++ks)
 #pragma unroll
         for (int a = 0; a < KP; ++a) {
           const kfrag k = kf(t4, ks, a);
@@ -115,9 +185,7 @@ template <typename ACT, int DH, int MT, int WK> struct Attend {
             for (int b = 0; b < NP; ++b)
               if (a + b <= 2) s[t][t4] = mma(k, q[t][b][ks], s[t][t4]);
         }
-      }
     }
-    bf16x8_t p[MT][NP][2], vis[MT][2];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       float mx = -INFINITY;
@@ -128,27 +196,20 @@ template <typename ACT, int DH, int MT, int WK> struct Attend {
           if (MASK && !seen(t, 16 * t4 + 4 * g + i)) s[t][t4][i] = -INFINITY;
           mx = fmaxf(mx, s[t][t4][i]);
         }
-      if (MASK && poison)
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          uint32_t x[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int key = 16 * (2 * w + (j >> 1)) + 4 * g + 2 * (j & 1);
-            x[j] = (seen(t, key) ? 0x3F80u : 0u) | (seen(t, key + 1) ? 0x3F800000u : 0u);
-          }
-          vis[t][w] = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
-        }
-      const float m_new = fmaxf(m[t], xor32_max(xor16_max(mx)) * scale2);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m[t] - ref);
-      m[t] = m_new;
-      if (__ballot(alpha != 1.f) != 0ull) {
+      mx *= scale2;
+      // The running maximum moves only when a score passes it by 2^8: until then
+      // probabilities stay below 2^8, which fp32 sums and bf16 operands carry
+      // as well, and a tile costs no exchange between lanes and no rescaling.
+      if (__ballot(mx > m[t] + 8.f) != 0ull) {
+        const float m_new = fmaxf(m[t], xor32_max(xor16_max(mx)));
+        const float alpha = __builtin_amdgcn_exp2f(m[t] - (m_new == -INFINITY ? 0.f : m_new));
+        m[t] = m_new;
         l[t] *= alpha;
         l1[t] *= alpha;
 #pragma unroll
         for (int u = 0; u < NU; ++u) o[t][u] *= alpha;
       }
+      const float ref = m[t] == -INFINITY ? 0.f : m[t];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         float x[8];
@@ -170,6 +231,9 @@ template <typename ACT, int DH, int MT, int WK> struct Attend {
 #pragma unroll
         for (int w = 0; w < 2; ++w) l1[t] = mma(ones, p[t][0][w], l1[t]);
     }
+  }
+  // o += P V: vf(column tile, half of the keys, part)
+  template <int KP, typename VF> __device__ __forceinline__ void values(VF vf, const bf16x8_t (&p)[MT][NP][2]) {
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
@@ -183,19 +247,47 @@ template <typename ACT, int DH, int MT, int WK> struct Attend {
             for (int b = 0; b < NP; ++b)
               if (a + b <= 2) o[t][u] = mma(v, p[t][b][w], o[t][u]);
         }
-    if (MASK && poison) {
-      // Some value of the tile is not finite (the operands above hold 0 there):
-      // it reaches the queries that see its key, and no other
+  }
+  // Where values of a tile are not finite the operands hold 0 in their place;
+  // bad(u, w) holds 1 there: NaN for the queries that see such a key, nothing for the others.
+  template <typename BAD, typename SEEN> __device__ __forceinline__ void poison(BAD bad, SEEN seen) {
 #pragma unroll
-      for (int u = 0; u < NU; ++u)
+    for (int t = 0; t < MT; ++t) {
+      bf16x8_t vis[2];
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          f32x4_t bad = {0.f, 0.f, 0.f, 0.f};
+      for (int w = 0; w < 2; ++w) {
+        uint32_t x[4];
 #pragma unroll
-          for (int w = 0; w < 2; ++w) bad = mma(vf(u, w, -1), vis[t][w], bad);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[t][u][i] = bad[i] > 0.f ? NAN : o[t][u][i];
+        for (int j = 0; j < 4; ++j) {
+          const int key = 16 * (2 * w + (j >> 1)) + 4 * g + 2 * (j & 1);
+          x[j] = (seen(t, key) ? 0x3F80u : 0u) | (seen(t, key + 1) ? 0x3F800000u : 0u);
         }
+        vis[w] = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+      }
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        f32x4_t b = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 2; ++w) b = mma(bad(u, w), vis[w], b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][u][i] = b[i] > 0.f ? NAN : o[t][u][i];
+      }
+    }
+  }
+  // folds another wave's (or split's) state of the same rows into this one
+  template <typename M, typename L, typename O> __device__ __forceinline__ void fold(M om, L ol, O oo) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      const float mo = om(t), mn = fmaxf(m[t], mo), ref = mn == -INFINITY ? 0.f : mn;
+      const float fa = __builtin_amdgcn_exp2f(m[t] - ref), fb = __builtin_amdgcn_exp2f(mo - ref);
+      m[t] = mn;
+      l[t] = l[t] * fa + ol(t) * fb;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) {
+        const f32x4_t x = oo(t, u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[t][u][i] = o[t][u][i] * fa + x[i] * fb;
+      }
     }
   }
 };
@@ -207,82 +299,106 @@ __device__ __forceinline__ uint32_t drop_codes(uint32_t w) {
   return w & ~((n >> 7) * 0xFFu);
 }
 
-template <typename ACT, int DH, int MT, int WK>
-__global__ __launch_bounds__(256) void k_cache_attend(CacheDev c, CacheAttend a) {
-  typedef Attend<ACT, DH, MT, WK> A;
-  constexpr int NP = A::NP, NS = A::NS, NU = A::NU;
-  typedef typename A::kfrag kfrag;
-  __shared__ f32x4_t fold_o[WK == 4 ? 2 : 1][WK == 4 ? MT * NU : 1][64];
-  __shared__ float fold_m[2][MT][64], fold_l[2][MT][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int h = blockIdx.y, G = c.H / c.KV;
-  int i, page0 = 0, page1 = INT32_MAX, item = 0;
-  bool tail = true, only = true;   // takes the exact blocks; is its row's one item
-  if (WK == 4) {
-    item = blockIdx.x;
-    if (item >= c.counts[0]) return;
-    const int4 w = c.items[item];
-    i = w.x;
-    page0 = w.y;
-    page1 = w.z;
-    tail = w.w != 0;
-    only = c.p_item[i + 1] - c.p_item[i] == 1;
-  } else {
-    i = blockIdx.x;
-  }
-  const int zb = gridDim.z - 1 - blockIdx.z;   // the groups with the most keys first
+// Query rows of a workgroup: a chunk of the query heads that share the
+// key/value head, of consecutive positions. ONE: a call's positions all at once
+// (they reach at most two blocks, as they are at most 64). Otherwise groups
+// that stay inside a block of 64 positions, so that a group has one block to see as
+// its rows came and none to see in part.
+struct Group {
+  int hc, gh, ppg, gpb;   // heads of a chunk, chunks, positions of a group, groups of a block
+};
+__host__ __device__ inline Group group_of(int G, int rows) {
+  Group x;
+  x.hc = G < rows ? G : rows;
+  x.gh = (G + x.hc - 1) / x.hc;
+  x.ppg = rows / x.hc;
+  if (x.ppg > CACHE_BLOCK) x.ppg = CACHE_BLOCK;
+  x.gpb = (CACHE_BLOCK + x.ppg - 1) / x.ppg;
+  return x;
+}
+inline int groups_of(int G, int rows, int P, bool one) {
+  const Group x = group_of(G, rows);
+  return one ? 1 : (CACHE_BLOCK - 1 + P + CACHE_BLOCK - 1) / CACHE_BLOCK * x.gpb * x.gh;
+}
+
+// Attention of a work item (a row of the batch and a range of its pages) for
+// one key/value head and one group of query rows. The NW waves share the
+// queries and take the pages round robin, each with its own running softmax,
+// folded at the end; the splits of a row are joined by the workgroup that
+// finishes last. The item with the row's last pages also takes the blocks that
+// the queries see as their rows came, from LDS. ONE: that item appends the
+// call's rows to the cache as well (ring, and pages of blocks that became
+// whole), so that a decoding step is one launch.
+template <typename ACT, int DH, int MT, int NW, bool ONE>
+__global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAttend a) {
+  typedef Rows<ACT, DH, MT> R;
+  constexpr int NP = R::NP, NS = R::NS, NU = R::NU, NT = 64 * NW;
+  constexpr int WIN = ONE ? 2 * CACHE_BLOCK : CACHE_BLOCK;   // rows as they came that a group may see
+  constexpr int LDK = DH + 16 / sizeof(ACT), LDV = WIN + 4;
+  typedef typename R::kfrag kfrag;
+  constexpr int FOLD = NW / 2;
+  struct Win {
+    ACT k[WIN][LDK];      // keys, row per position
+    ACT v[DH][LDV];       // values, row per column
+  };
+  struct Fold {
+    f32x4_t o[FOLD][MT * NU][64];
+    float m[FOLD][MT][64], l[FOLD][MT][64];
+  };
+  union Shared {
+    Win win;
+    Fold fold;
+  };
+  __shared__ __align__(16) char shared[sizeof(Shared)];
+  __shared__ float top[2][NW];
+  __shared__ int last_of_row;
+  Win &win = *(Win *)shared;
+  Fold &fold = *(Fold *)shared;
+
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, rr = lane & 15, g = lane >> 4;
+  const int h = blockIdx.y, G = c.H / c.KV, item = blockIdx.x;
+  if (item >= c.counts[0]) return;
+  const int4 it = c.items[item];
+  const int i = it.x, slot = it.w;   // slot of this split's partial state, -1: the row's one item
   const int cnt = c.p_count[i], start = c.p_start[i], seq = c.p_seq[i];
-  const int r0 = (WK == 4 ? zb : zb * 4 + wave) * 16 * MT;
   const size_t head0 = (size_t)h * G * DH;
   ACT *const O = (ACT *)a.o;
+  // this group: query heads hd0 .. + hn - 1 of positions p0 .. + pn - 1
+  const Group grp = group_of(G, 16 * MT);
+  int hd0 = 0, hn = G, p0 = start, pn = cnt, z = 0;
+  if (!ONE) {
+    z = gridDim.z - 1 - blockIdx.z;   // the groups with the most keys first
+    const int gh = z % grp.gh, sub = z / grp.gh % grp.gpb, blk = z / grp.gh / grp.gpb;
+    hd0 = gh * grp.hc;
+    hn = min(grp.hc, G - hd0);
+    const int b0 = (start / CACHE_BLOCK + blk) * CACHE_BLOCK, lo = b0 + sub * grp.ppg;
+    p0 = max(start, lo);
+    pn = min(start + cnt, min(lo + grp.ppg, b0 + CACHE_BLOCK)) - p0;
+  }
   if (cnt <= 0) {
-    if (a.zero)
-      for (int x = lane; x < 16 * MT * DH; x += 64) {
-        const int r = r0 + x / DH;
-        if (r < a.P * G && (WK == 1 || wave == 0))
-          O[((size_t)i * a.P + r / G) * a.ldo + head0 + (r % G) * DH + x % DH] = 0;
-      }
+    if (a.zero && (ONE || z == 0))
+      for (int x = tid; x < a.P * G * DH; x += NT)
+        O[((size_t)i * a.P + x / (G * DH)) * a.ldo + head0 + x % (G * DH)] = 0;
     return;
   }
-  const int R = cnt * G;
-  if (r0 >= R) return;   // (no barrier ahead that other waves would wait at: WK == 4 leaves as a whole)
-  A s;
-  s.rr = lane & 15;
-  s.g = lane >> 4;
+  if (pn <= 0) return;   // (the group's position range of this row is empty: for all its splits)
+  const int end = start + cnt;
+  const int ba = p0 / CACHE_BLOCK, bb = (p0 + pn - 1) / CACHE_BLOCK;
+  const bool tail = it.z >= (end - 1) / CACHE_BLOCK;
+  // the split that takes the group's own block: the one whose pages it is among,
+  // or would follow
+  const bool mine = ONE ? tail : (it.y <= ba && ba < it.z) || (tail && ba >= it.z);
+  R s;
+  s.g = g;
   s.scale2 = a.scale * LOG2E;
-  const int g = s.g, rr = s.rr;
-  const int bb = (start + (min(r0 + 16 * MT, R) - 1) / G) / CACHE_BLOCK;   // block of the last query
-  const int ba = (start + r0 / G) / CACHE_BLOCK;                           // and of the first
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const int r = min(r0 + 16 * t + rr, R - 1);   // (rows past the last repeat it and are not stored)
-    s.pos[t] = start + r / G;
-    const ACT *qp = (const ACT *)a.q + ((size_t)i * a.P + r / G) * a.ldq + head0 + (r % G) * DH;
+    const int r = min(16 * t + rr, pn * hn - 1);   // (rows past the last repeat it and are not stored)
+    const int p = r / hn, hd = hd0 + r - p * hn;
+    s.pos[t] = p0 + p;
+    const ACT *qp = (const ACT *)a.q + ((size_t)i * a.P + (p0 - start + p)) * a.ldq + head0 + hd * DH;
 #pragma unroll
-    for (int ks = 0; ks < NS; ++ks) {
-      if constexpr (DH >= 32) {
-        if constexpr (NP == 1) {
-          s.q[t][0][ks] = *(const bf16x8_t *)(qp + 32 * ks + 8 * g);
-        } else {
-          float x[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = qp[32 * ks + 8 * g + j];
-          bf16x8_t part[NP];
-          split8<NP>(x, part);
-#pragma unroll
-          for (int b = 0; b < NP; ++b) s.q[t][b][ks] = part[b];
-        }
-      } else if constexpr (NP == 1) {
-        s.q[t][0][ks] = *(const short4_t *)(qp + 4 * g);
-      } else {
-        float x[8] = {qp[4 * g], qp[4 * g + 1], qp[4 * g + 2], qp[4 * g + 3], 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int b = 0; b < NP; ++b) {
-          const uint4 w = take8(x, true);
-          s.q[t][b][ks] = __builtin_bit_cast(short4_t, make_uint2(w.x, w.y));
-        }
-      }
-    }
+    for (int ks = 0; ks < NS; ++ks) load_k<ACT, DH>(qp + (DH >= 32 ? 32 * ks + 8 * g : 4 * g), [&](int b) -> kfrag & { return s.q[t][b][ks]; });
     s.m[t] = -INFINITY;
     s.l[t] = 0.f;
     s.l1[t] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
@@ -290,184 +406,237 @@ __global__ __launch_bounds__(256) void k_cache_attend(CacheDev c, CacheAttend a)
     for (int u = 0; u < NU; ++u) s.o[t][u] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
   }
 
-  // ---- pages: blocks before the last query's -----------------------------
-  const int32_t *table = c.table + (size_t)seq * c.NP;
+  // ---- rows of the queries' own blocks, into LDS (and the cache) ------------
   const size_t layer0 = (size_t)a.layer * c.n_pages;
-  const int j_end = min(page1, bb);
-  for (int j = page0 + (WK == 4 ? wave : 0); j < j_end; j += WK) {
-    const size_t tile = (layer0 + table[j]) * c.KV + h;
-    const uint4 *kp = (const uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)) + lane;
-    uint32_t kw[NU][4], vw[NU][4];
+  const int32_t *table = c.table + (size_t)seq * c.NP;
+  const int j0 = it.y, j1 = min(it.z, ba);
+  auto tile_of = [&](int page) { return (layer0 + page) * c.KV + h; };
+  auto load_side = [&](uint4 (&w)[NU], size_t tile, int side) {
+    const uint4 *p = (const uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)) + side * (64 * NU) + lane;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      const uint4 x = kp[64 * u], y = kp[64 * (NU + u)];
-      kw[u][0] = x.x, kw[u][1] = x.y, kw[u][2] = x.z, kw[u][3] = x.w;
-      vw[u][0] = y.x, vw[u][1] = y.y, vw[u][2] = y.z, vw[u][3] = y.w;
-    }
-    const float ks = c.scales[tile * 2], vs = c.scales[tile * 2 + 1];
-    auto kf = [&](int t4, int s2, int) -> kfrag {
-      if constexpr (DH >= 32) {
-        const int f = t4 * NS + s2;
-        return dec8(kw[f >> 1][2 * (f & 1)], kw[f >> 1][2 * (f & 1) + 1], ks);
-      } else {
-        return dec4(kw[0][t4], ks);
-      }
-    };
-    if (j < ba) {   // every query sees it
-      auto vf = [&](int u, int w, int) { return dec8(vw[u][2 * w], vw[u][2 * w + 1], vs); };
-      s.template tile<1, false>(kf, vf, [](int, int) { return true; }, false);
+    for (int u = 0; u < NU; ++u) w[u] = p[64 * u];
+  };
+  auto word = [](const uint4 &x, int n) { return n == 0 ? x.x : n == 1 ? x.y : n == 2 ? x.z : x.w; };
+  auto k_codes = [&](const uint4 (&w)[NU], float sc, int t4, int ks) -> kfrag {
+    if constexpr (DH >= 32) {
+      const int f = t4 * NS + ks;
+      return dec8(word(w[f >> 1], 2 * (f & 1)), word(w[f >> 1], 2 * (f & 1) + 1), sc);
     } else {
-      uint32_t any = 0;
-#pragma unroll
-      for (int u = 0; u < NU; ++u)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) any |= nan_codes(vw[u][x]);
-      auto vf = [&](int u, int w, int part) {
-        const uint32_t x = vw[u][2 * w], y = vw[u][2 * w + 1];
-        if (part >= 0) return dec8(drop_codes(x), drop_codes(y), vs);
-        // 1.0 (code 0x38) where a code is NaN
-        return dec8((nan_codes(x) >> 7) * 0x38u, (nan_codes(y) >> 7) * 0x38u, 1.f);
-      };
-      s.template tile<1, true>(kf, vf, [&](int t, int) { return s.pos[t] / CACHE_BLOCK > j; }, __ballot(any != 0) != 0ull);
+      return dec4(word(w[0], t4), sc);
     }
-  }
-
-  // ---- the queries' own blocks, as their rows came -----------------------
-  if (tail) {
-    const bool ring_all = a.P <= CACHE_BLOCK;   // the append has put every row of the call into the ring
-    const int end = start + cnt;
+  };
+  int any_bad = 0;
+  if (mine) {
+    const int base = ba * CACHE_BLOCK, n = min(end - base, WIN);
     const ACT *ring = (const ACT *)c.tails + (((size_t)a.layer * c.S + seq) * c.KV + h) * 2 * CACHE_RING * DH;
     const ACT *stash = (const ACT *)c.stash + ((size_t)i * c.KV + h) * 2 * CACHE_BLOCK * DH;
-    const CacheRows &R2 = a.kv;
-    auto k_row = [&](int p) -> const ACT * {
-      if (ring_all) return ring + (p % CACHE_RING) * DH;
-      if (p < start) return stash + (p % CACHE_BLOCK) * DH;
-      return (const ACT *)R2.k + i * R2.k_sb + (size_t)(p - start) * R2.k_sp + h * R2.k_sh;
-    };
-    auto v_el = [&](int p, int j) -> ACT {
-      if (ring_all) return ring[(CACHE_RING + p % CACHE_RING) * DH + j];
-      if (p < start) return stash[(CACHE_BLOCK + p % CACHE_BLOCK) * DH + j];
-      const ACT *V = (const ACT *)R2.v;
-      const int pn = p - start;
-      return R2.v_blocked ? V[i * R2.v_sb + h * R2.v_sh + (size_t)(pn >> 3) * 8 * DH + j * 8 + (pn & 7)]
-                          : V[i * R2.v_sb + (size_t)pn * R2.v_sp + h * R2.v_sh + j];
-    };
-    for (int b = ba; b <= bb; ++b) {
-      if (WK == 4 && ((b - ba + j_end) & 3) != wave) continue;
-      const int base = b * CACHE_BLOCK;
-      kfrag kr[4][NP][NS];
-#pragma unroll
-      for (int t4 = 0; t4 < 4; ++t4) {
-        const ACT *kp = k_row(min(base + 16 * t4 + rr, end - 1));
-#pragma unroll
-        for (int k2 = 0; k2 < NS; ++k2) {
-          if constexpr (DH >= 32) {
-            if constexpr (NP == 1) {
-              kr[t4][0][k2] = *(const bf16x8_t *)(kp + 32 * k2 + 8 * g);
-            } else {
-              float x[8];
-#pragma unroll
-              for (int j = 0; j < 8; ++j) x[j] = kp[32 * k2 + 8 * g + j];
-              bf16x8_t part[NP];
-              split8<NP>(x, part);
-#pragma unroll
-              for (int n = 0; n < NP; ++n) kr[t4][n][k2] = part[n];
-            }
-          } else if constexpr (NP == 1) {
-            kr[t4][0][k2] = *(const short4_t *)(kp + 4 * g);
-          } else {
-            float x[8] = {kp[4 * g], kp[4 * g + 1], kp[4 * g + 2], kp[4 * g + 3], 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int n = 0; n < NP; ++n) {
-              const uint4 w = take8(x, true);
-              kr[t4][n][k2] = __builtin_bit_cast(short4_t, make_uint2(w.x, w.y));
-            }
-          }
-        }
+    const bool in_ring = a.P <= CACHE_BLOCK;   // rows from before the call (longer ones have moved them to the stash)
+    constexpr int C8 = DH / 8;                 // pieces of 8 elements of a row
+    const CacheRows &src = a.kv;
+    int bad = 0;
+    for (int x = tid; x < WIN * C8; x += NT) {
+      const int row = x / C8, j = (x - row * C8) * 8, pos = base + row;
+      const ACT *kp, *vp;
+      bool blocked = false;
+      if (pos < start) {
+        const ACT *from = in_ring ? ring + (pos % CACHE_RING) * DH : stash + row * DH;
+        kp = from + j;
+        vp = from + (in_ring ? CACHE_RING : CACHE_BLOCK) * DH + j;
+      } else {
+        const int pr = min(pos, end - 1) - start;
+        kp = (const ACT *)src.k + i * src.k_sb + (size_t)pr * src.k_sp + h * src.k_sh + j;
+        blocked = src.v_blocked != 0;
+        vp = (const ACT *)src.v + i * src.v_sb + h * src.v_sh +
+             (blocked ? (size_t)(pr >> 3) * 8 * DH + j * 8 + (pr & 7) : (size_t)pr * src.v_sp + j);
       }
-      bf16x8_t vr[NU][2][NP], vbad[NU][2];
-      bool any = false;
+      ACT kk[8], vv[8];
+      const bool in = row < n;
+      load8(kk, kp);
+      if (blocked) {
 #pragma unroll
-      for (int u = 0; u < NU; ++u)
+        for (int e = 0; e < 8; ++e) vv[e] = vp[8 * e];
+      } else {
+        load8(vv, vp);
+      }
+      store8(&win.k[row][j], kk);
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          float x[8];
-          uint32_t bad[8];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int p = base + 16 * (2 * w + (j >> 2)) + 4 * g + (j & 3);
-            const ACT e = v_el(min(p, end - 1), 16 * u + rr);
-            x[j] = p < end ? ld(&e, 0) : 0.f;
-            const bool nf = !(fabsf(x[j]) < INFINITY);
-            any |= nf;
-            bad[j] = nf ? 0x3F80u : 0u;
-            x[j] = nf ? 0.f : x[j];
-          }
-          split8<NP>(x, vr[u][w]);
-          vbad[u][w] = __builtin_bit_cast(bf16x8_t, make_uint4(bad[0] | bad[1] << 16, bad[2] | bad[3] << 16,
-                                                               bad[4] | bad[5] << 16, bad[6] | bad[7] << 16));
+      for (int e = 0; e < 8; ++e) {
+        win.v[j + e][row] = in ? vv[e] : (ACT)0;
+        bad |= in && not_finite(ld(&vv[e], 0));
+      }
+      if (ONE && in && pos >= start) {
+        ACT *to = (ACT *)ring + (pos % CACHE_RING) * DH + j;
+        store8(to, kk);
+        store8(to + CACHE_RING * DH, vv);
+      }
+    }
+    any_bad = __syncthreads_or(bad);
+    if constexpr (ONE) {
+      if (n >= CACHE_BLOCK) {   // the first block is whole: its page
+        float m[2] = {0.f, 0.f};
+        for (int x = tid; x < CACHE_BLOCK * DH; x += NT) {
+          const float kf = fabsf(ld(&win.k[x / DH][x % DH], 0)), vf = fabsf(ld(&win.v[x / CACHE_BLOCK][x % CACHE_BLOCK], 0));
+          m[0] = kf < INFINITY ? fmaxf(m[0], kf) : m[0];
+          m[1] = vf < INFINITY ? fmaxf(m[1], vf) : m[1];
         }
-      s.template tile<NP, true>(
-          [&](int t4, int k2, int part) { return kr[t4][part][k2]; },
-          [&](int u, int w, int part) { return part < 0 ? vbad[u][w] : vr[u][w][part < 0 ? 0 : part]; },
-          [&](int t, int key) { return s.pos[t] / CACHE_BLOCK == b && base + key <= s.pos[t]; }, __ballot(any) != 0ull);
+        m[0] = lanes_max(m[0]);
+        m[1] = lanes_max(m[1]);
+        if (lane == 0) top[0][wave] = m[0], top[1][wave] = m[1];
+        __syncthreads();
+        const size_t tile = tile_of(table[ba]);
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+          float mx = 0.f;
+#pragma unroll
+          for (int w = 0; w < NW; ++w) mx = fmaxf(mx, top[side][w]);
+          const int e = scale_exp(mx);
+          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+          if (tid == 0) c.scales[tile * 2 + side] = __uint_as_float((uint32_t)(127 + e) << 23);
+          for (int x = tid; x < CACHE_BLOCK * DH / 16; x += NT) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float f[4];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                int key, col;
+                if (side == 0) key_at<DH>(x >> 6, x & 63, 4 * q + y, key, col);
+                else value_at(x >> 6, x & 63, 4 * q + y, key, col);
+                f[y] = side == 0 ? ld(&win.k[key][col], 0) : ld(&win.v[col][key], 0);
+              }
+              w[q] = codes4(f[0], f[1], f[2], f[3], inv);
+            }
+            ((uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)))[side * (64 * NU) + x] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        __syncthreads();   // (the page is read below, by waves of this workgroup)
+      }
     }
   }
 
-  // ---- sums over the lane groups, then over the waves ---------------------
+  // ---- the pages that every query sees ------------------------------------
+  for (int jc = j0 + wave; jc < j1; jc += 64 * NW) {
+    // page ids and scales of the wave's next 64 pages, one per lane
+    const int jl = min(jc + lane * NW, j1 - 1), n = min(64, (j1 - jc + NW - 1) / NW);
+    const int id = table[jl];
+    const float2 sc = *(const float2 *)(c.scales + tile_of(id) * 2);
+    uint4 kw[NU], vw[NU], kn[NU];
+    load_side(kw, tile_of(__builtin_amdgcn_readlane(id, 0)), 0);
+    for (int x = 0; x < n; ++x) {
+      const size_t tile = tile_of(__builtin_amdgcn_readlane(id, x));
+      const float ks = lane_val(sc.x, x), vs = lane_val(sc.y, x);
+      load_side(vw, tile, 1);
+      load_side(kn, tile_of(__builtin_amdgcn_readlane(id, min(x + 1, n - 1))), 0);
+      bf16x8_t p[MT][NP][2];
+      s.template scores<1, false>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
+                                  [](int, int) { return true; }, p);
+      s.template values<1>([&](int u, int w, int) { return dec8(word(vw[u], 2 * w), word(vw[u], 2 * w + 1), vs); }, p);
+#pragma unroll
+      for (int u = 0; u < NU; ++u) kw[u] = kn[u];
+    }
+  }
+
+  // ---- the queries' own blocks, as their rows came -------------------------
+  if (mine) {
+    // step 0: block ba as it came; ONE, past its border: 1: block bb as it came, 2: block ba's page
+    const int steps = ONE && bb > ba ? 3 : 1;
+    for (int st = (wave + NW - (max(j1 - j0, 0)) % NW) % NW; st < steps; st += NW) {
+      bf16x8_t p[MT][NP][2];
+      if (ONE && st == 2) {
+        const size_t tile = tile_of(table[ba]);
+        uint4 kw[NU], vw[NU];
+        load_side(kw, tile, 0);
+        load_side(vw, tile, 1);
+        const float ks = c.scales[tile * 2], vs = c.scales[tile * 2 + 1];
+        auto seen = [&](int t, int) { return s.pos[t] / CACHE_BLOCK > ba; };
+        s.template scores<1, true>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); }, seen, p);
+        s.template values<1>([&](int u, int w, int) {
+          return dec8(drop_codes(word(vw[u], 2 * w)), drop_codes(word(vw[u], 2 * w + 1)), vs); }, p);
+        if (any_bad)   // 1.0 (code 0x38) where a code is NaN
+          s.poison([&](int u, int w) {
+            return dec8((nan_codes(word(vw[u], 2 * w)) >> 7) * 0x38u, (nan_codes(word(vw[u], 2 * w + 1)) >> 7) * 0x38u, 1.f); }, seen);
+        continue;
+      }
+      const int b = ba + st, w0 = st * CACHE_BLOCK;
+      auto seen = [&](int t, int key) { return s.pos[t] / CACHE_BLOCK == b && b * CACHE_BLOCK + key <= s.pos[t]; };
+      kfrag kr[NP][NS];
+      s.template scores<NP, true>([&](int t4, int k2, int part) {
+        if (part == 0)
+          load_k<ACT, DH>(&win.k[w0 + 16 * t4 + rr][DH >= 32 ? 32 * k2 + 8 * g : 4 * g], [&](int x) -> kfrag & { return kr[x][k2]; });
+        return kr[part][k2];
+      }, seen, p);
+      bf16x8_t vr[NP];
+      s.template values<NP>([&](int u, int w, int part) {
+        if (part == 0) value8<NP>(&win.v[16 * u + rr][w0 + 32 * w + 4 * g], any_bad != 0, vr);
+        return vr[part];
+      }, p);
+      if (any_bad)
+        s.poison([&](int u, int w) { return bad8(&win.v[16 * u + rr][w0 + 32 * w + 4 * g]); }, seen);
+    }
+    __syncthreads();   // (the window's memory is the folding's next)
+  }
+
+  // ---- sums over the lane groups, then over the waves ----------------------
 #pragma unroll
   for (int t = 0; t < MT; ++t) s.l[t] = NP == 1 ? s.l1[t][0] : xor32_sum(xor16_sum(s.l[t]));
-  if constexpr (WK == 4) {
 #pragma unroll
-    for (int half = 2; half > 0; half >>= 1) {
-      if (wave >= half && wave < 2 * half) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          fold_m[wave - half][t][lane] = s.m[t];
-          fold_l[wave - half][t][lane] = s.l[t];
-#pragma unroll
-          for (int u = 0; u < NU; ++u) fold_o[wave - half][t * NU + u][lane] = s.o[t][u];
-        }
-      }
-      __syncthreads();
-      if (wave < half) {
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          const float mo = fold_m[wave][t][lane], mn = fmaxf(s.m[t], mo), ref = mn == -INFINITY ? 0.f : mn;
-          const float fa = __builtin_amdgcn_exp2f(s.m[t] - ref), fb = __builtin_amdgcn_exp2f(mo - ref);
-          s.m[t] = mn;
-          s.l[t] = s.l[t] * fa + fold_l[wave][t][lane] * fb;
-#pragma unroll
-          for (int u = 0; u < NU; ++u) {
-            const f32x4_t x = fold_o[wave][t * NU + u][lane];
-#pragma unroll
-            for (int i2 = 0; i2 < 4; ++i2) s.o[t][u][i2] = s.o[t][u][i2] * fa + x[i2] * fb;
-          }
-        }
-      }
-      __syncthreads();
-    }
-    if (wave != 0) return;
-    if (!only) {
-      // [item][head][group][m, l, o][64]: what k_cache_join reads lane by lane
-      constexpr int N = 2 * MT + 4 * MT * NU;
-      float *pp = c.part + (((size_t)item * c.KV + h) * gridDim.z + zb) * N * 64 + lane;
+  for (int half = NW / 2; half > 0; half >>= 1) {
+    if (wave >= half && wave < 2 * half) {
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        pp[64 * t] = s.m[t];
-        pp[64 * (MT + t)] = s.l[t];
+        fold.m[wave - half][t][lane] = s.m[t];
+        fold.l[wave - half][t][lane] = s.l[t];
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
-#pragma unroll
-          for (int i2 = 0; i2 < 4; ++i2) pp[64 * (2 * MT + 4 * (t * NU + u) + i2)] = s.o[t][u][i2];
+        for (int u = 0; u < NU; ++u) fold.o[wave - half][t * NU + u][lane] = s.o[t][u];
       }
-      return;
+    }
+    __syncthreads();
+    if (wave < half)
+      s.fold([&](int t) { return fold.m[wave][t][lane]; }, [&](int t) { return fold.l[wave][t][lane]; },
+             [&](int t, int u) { return fold.o[wave][t * NU + u][lane]; });
+    if (half > 1) __syncthreads();
+  }
+  if (wave != 0) return;
+  if (slot >= 0) {
+    // [slot][head][group][o, m, l][64]: lane by lane
+    constexpr int N = 4 * MT * NU + 2 * MT;
+    const int Z = gridDim.z, it0 = c.p_item[i], ns = c.p_item[i + 1] - it0, s0 = slot - (item - it0);
+    auto part = [&](int sl) { return c.part + (((size_t)sl * c.KV + h) * Z + z) * N * 64; };
+    float *pp = part(slot);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+#pragma unroll
+      for (int u = 0; u < NU; ++u) ((f32x4_t *)pp)[64 * (t * NU + u) + lane] = s.o[t][u];
+      pp[64 * (4 * MT * NU + t) + lane] = s.m[t];
+      pp[64 * (4 * MT * NU + MT + t) + lane] = s.l[t];
+    }
+    __threadfence();
+    int *arrived = c.joins + ((size_t)i * c.KV + h) * Z + z;
+    int before = 0;
+    if (lane == 0) before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    before = __builtin_amdgcn_readfirstlane(before);
+    if (before != ns - 1) return;
+    __threadfence();
+    if (lane == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    // the splits in order, whoever comes last
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      s.m[t] = -INFINITY;
+      s.l[t] = 0.f;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) s.o[t][u] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+    }
+    for (int x = 0; x < ns; ++x) {
+      const float *pq = part(s0 + x);
+      s.fold([&](int t) { return pq[64 * (4 * MT * NU + t) + lane]; },
+             [&](int t) { return pq[64 * (4 * MT * NU + MT + t) + lane]; },
+             [&](int t, int u) { return ((const f32x4_t *)pq)[64 * (t * NU + u) + lane]; });
     }
   }
   // ---- normalise and store: lane (rr, g) holds columns 16 u + 4 g .. + 3 of query rr ----
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
-    const int r = r0 + 16 * t + rr;
+    const int r = 16 * t + rr;
     float f = 1.f, L = s.l[t];
     if (a.sink) {   // one more key of score 0 and value 0
       const float ms = fmaxf(s.m[t], 0.f);
@@ -475,8 +644,9 @@ __global__ __launch_bounds__(256) void k_cache_attend(CacheDev c, CacheAttend a)
       L = L * f + __builtin_amdgcn_exp2f(-ms);
     }
     f = f / L;
-    if (r >= R) continue;
-    ACT *op = O + ((size_t)i * a.P + r / G) * a.ldo + head0 + (r % G) * DH + 4 * g;
+    if (r >= pn * hn) continue;
+    const int p = r / hn, hd = hd0 + r - p * hn;
+    ACT *op = O + ((size_t)i * a.P + (p0 - start + p)) * a.ldo + head0 + hd * DH + 4 * g;
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
       if constexpr (NP == 1)
@@ -487,105 +657,64 @@ __global__ __launch_bounds__(256) void k_cache_attend(CacheDev c, CacheAttend a)
   }
 }
 
-// joins the splits of a (row, head, group of query rows): one wave each
-template <typename ACT, int DH, int MT>
-__global__ __launch_bounds__(64) void k_cache_join(CacheDev c, CacheAttend a) {
-  constexpr int NU = DH / 16, N = 2 * MT + 4 * MT * NU;
-  const int i = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, rr = lane & 15, g = lane >> 4, G = c.H / c.KV;
-  const int it0 = c.p_item[i], it1 = c.p_item[i + 1], R = c.p_count[i] * G, r0 = blockIdx.z * 16 * MT;
-  if (it1 - it0 <= 1 || r0 >= R) return;
-  const size_t step = (size_t)c.KV * gridDim.z * N * 64;
-  const float *p0 = c.part + (((size_t)it0 * c.KV + h) * gridDim.z + blockIdx.z) * N * 64 + lane;
-  for (int t = 0; t < MT; ++t) {
-    float m = -INFINITY, l = 0.f;
-    for (int x = it0; x < it1; ++x) m = fmaxf(m, p0[(x - it0) * step + 64 * t]);
-    if (a.sink) m = fmaxf(m, 0.f);
-    f32x4_t o[NU];
-#pragma unroll
-    for (int u = 0; u < NU; ++u) o[u] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-    for (int x = it0; x < it1; ++x) {
-      const float *pp = p0 + (x - it0) * step;
-      const float f = __builtin_amdgcn_exp2f(pp[64 * t] - m);
-      l += pp[64 * (MT + t)] * f;
-#pragma unroll
-      for (int u = 0; u < NU; ++u)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[u][e] += pp[64 * (2 * MT + 4 * (t * NU + u) + e)] * f;
-    }
-    if (a.sink) l += __builtin_amdgcn_exp2f(-m);
-    const int r = r0 + 16 * t + rr;
-    if (r >= R) continue;
-    const float f = 1.f / l;
-    ACT *op = (ACT *)a.o + ((size_t)i * a.P + r / G) * a.ldo + (size_t)(h * G + r % G) * DH + 4 * g;
-#pragma unroll
-    for (int u = 0; u < NU; ++u) {
-      if constexpr (sizeof(ACT) == 2)
-        *(uint2 *)(op + 16 * u) = make_uint2(pk2bf(o[u][0] * f, o[u][1] * f), pk2bf(o[u][2] * f, o[u][3] * f));
-      else
-        *(f32x4_t *)(op + 16 * u) = o[u] * f;
-    }
-  }
+// Tiles of 16 query rows of a workgroup for R rows in all: up to four, two
+// where four do not fit the registers (outputs of d_head 128; fp32's three
+// parts of queries and probabilities).
+constexpr int max_tiles(int dh, bool bf16) { return dh <= (bf16 ? 64 : 32) ? 4 : 2; }
+int tiles_of(const CacheDev &c, long R) { return std::min(R <= 16 ? 1 : R <= 32 ? 2 : 4, max_tiles(c.dh, c.bf16)); }
+
+// all of a call's query rows in one group
+bool one_group(const CacheDev &c, int P) {
+  return P <= CACHE_BLOCK && (long)P * (c.H / c.KV) <= 16 * max_tiles(c.dh, c.bf16);
 }
 
-// query tiles of a wave for R rows
-int tiles_of(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 4; }
+int call_groups(const CacheDev &c, int P) {
+  const int G = c.H / c.KV;
+  const bool one = one_group(c, P);
+  return groups_of(G, 16 * (one ? tiles_of(c, (long)P * G) : max_tiles(c.dh, c.bf16)), P, one);
+}
 
 }  // namespace
 
-// Rows of queries enough to fill the chip with four waves of their own each
-// take the key range whole; otherwise the waves of a workgroup, and workgroups,
-// split the keys.
-static bool by_rows(const CacheDev &c, int B, int P) {
-  const long R = (long)P * (c.H / c.KV);
-  return R > 64 && (long)B * c.KV * ((R + 127) / 128) >= 256;
-}
-
 int cache_split_target(const CacheDev &c, int B, int P) {
-  if (by_rows(c, B, P)) return 0;
-  const long R = (long)P * (c.H / c.KV), groups = (R + 63) / 64;
-  const long per = c.KV * groups;
-  if (B * per >= CACHE_SPLIT_WGS) return 0;
-  return (int)((CACHE_SPLIT_WGS + per - 1) / per);
+  const long per = (long)c.KV * call_groups(c, P);
+  return per > CACHE_SPLIT_WGS || B * per > CACHE_JOINS ? 0 : (int)(CACHE_SPLIT_WGS / per);
 }
 
-// items of a call: at most one per row and split_target more
-int cache_max_items(int S, int KV) { return S + CACHE_SPLIT_WGS / KV + 2; }
+// a row, and for a split batch about three times the target more
+int cache_max_items(int S, int KV) { return S + 3 * (CACHE_SPLIT_WGS / KV + 1) + 2; }
 
-// Partials of a split call: items x heads x groups of query rows slots, fewer
-// than 3 CACHE_SPLIT_WGS (both the rows' own and split_target's are at most
-// that many, and a group more), and no more than the items that pages of
-// splits of four give. A slot holds maximum, sum and output of up to four tiles
-// of 16 queries, lane by lane.
+// Partial states: a row of t pages in pieces of C >= pages / (3 target) takes
+// ceil(t / C) < 2 t / C slots, so all rows at most 6 target, each of heads x
+// groups states; target x heads x groups <= CACHE_SPLIT_WGS. A state is
+// output, maximum and sum of up to four tiles of 16 query rows, lane by lane.
 size_t cache_part_floats(const CacheDev &c) {
-  const size_t groups = ((size_t)c.max_events * (c.H / c.KV) + 63) / 64;
-  const size_t most = (size_t)c.KV * groups * ((size_t)c.S + (size_t)c.S * c.NP / 4 + 1);
-  return std::min<size_t>(3 * CACHE_SPLIT_WGS, most) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
+  const size_t groups = (size_t)call_groups(c, c.max_events);
+  const size_t few = c.KV * groups * ((size_t)c.S + (size_t)c.S * c.NP / CACHE_MIN_PIECE);
+  return std::min<size_t>(6 * CACHE_SPLIT_WGS, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
 }
 
 void launch_cache_attend(const CacheDev &c, const CacheAttend &a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
-  const int G = c.H / c.KV;
-  const long R = (long)a.P * G;
+  const long R = (long)a.P * (c.H / c.KV);
+  const bool one = one_group(c, a.P);
+  const int target = cache_split_target(c, a.B, a.P), items = a.B + (target ? 3 * target + 1 : 0);
+  if (!one) launch_cache_append(c, a.layer, a.B, a.P, a.kv, st);
   auto go = [&](auto act, auto width) {
     typedef decltype(act) ACT;
     constexpr int DH = decltype(width)::value;
-    if (by_rows(c, a.B, a.P)) {
-      constexpr int MT = 2;
-      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 1>), dim3(a.B, c.KV, (unsigned)((R + 64 * MT - 1) / (64 * MT))),
-                            dim3(256), 0, st, ev0, ev1, 0, c, a);
-      return;
-    }
-    const int target = cache_split_target(c, a.B, a.P), items = a.B + target;
-    auto split = [&](auto mt) {
+    auto launch = [&](auto mt, auto is_one) {
       constexpr int MT = decltype(mt)::value;
-      const unsigned groups = (unsigned)((R + 16 * MT - 1) / (16 * MT));
-      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 4>), dim3(items, c.KV, groups), dim3(256), 0, st, ev0, ev1, 0,
-                            c, a);
-      if (target) k_cache_join<ACT, DH, MT><<<dim3(a.B, c.KV, groups), 64, 0, st>>>(c, a);
+      constexpr bool ONE = decltype(is_one)::value;
+      constexpr int NW = ONE && DH * (int)sizeof(ACT) <= 128 && MT < 4 ? 8 : 4;
+      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, NW, ONE>), dim3(items, c.KV, call_groups(c, a.P)), dim3(64 * NW),
+                            0, st, ev0, ev1, 0, c, a);
     };
-    const int mt = tiles_of((int)std::min<long>(R, 64));
-    if (mt == 1) split(std::integral_constant<int, 1>{});
-    else if (mt == 2) split(std::integral_constant<int, 2>{});
-    else split(std::integral_constant<int, 4>{});
+    constexpr int MOST = max_tiles(DH, sizeof(ACT) == 2);
+    const int mt = tiles_of(c, R);
+    if (!one) launch(std::integral_constant<int, MOST>{}, std::false_type{});
+    else if (mt == 1) launch(std::integral_constant<int, 1>{}, std::true_type{});
+    else if (mt == 2) launch(std::integral_constant<int, 2>{}, std::true_type{});
+    else launch(std::integral_constant<int, MOST>{}, std::true_type{});
   };
   auto widths = [&](auto act) {
     if (c.dh == 16) go(act, std::integral_constant<int, 16>{});
