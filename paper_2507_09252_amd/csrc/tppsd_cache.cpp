@@ -86,9 +86,8 @@ size_t view(CacheDev *c, char *ws, Entry *entries) {
   take(c->p_seq, S * 4);
   take(c->p_start, S * 4);
   take(c->p_count, S * 4);
-  take(c->p_item, (S + 1) * 4);
   c->max_items = cache_max_items(c->S, c->KV);
-  take(c->items, (size_t)c->max_items * 16);
+  take(c->items, (size_t)c->max_items * sizeof(CacheItem));
   take(c->part, cache_part_floats(*c) * 4);
   take(c->joins, CACHE_JOINS * 4);
   take(c->stash, S * KV * 2 * CACHE_BLOCK * dh * e);

@@ -20,10 +20,20 @@ constexpr int CACHE_RING = 128;   // tail rows: two blocks
 // Least exponent of a scale: 2^-100 keeps every code's value, and its product
 // with the reciprocal scale, a normal fp32 (and bf16) number
 constexpr int CACHE_E_MIN = -100;
-// Workgroups of the attention that make a full chip (one per CU), the fewest
-// pages of a piece of a row, and the most (row, head, group) triples of a batch
-// whose rows are split
-constexpr int CACHE_SPLIT_WGS = 256, CACHE_MIN_PIECE = 8, CACHE_JOINS = 4096;
+// Waves of the attention that make a full chip (two per SIMD), the fewest pages
+// of a piece of a row, and the most (row, head, group) triples of a batch whose
+// rows are split
+constexpr int CACHE_SPLIT_WAVES = 2048, CACHE_MIN_PIECE = 8, CACHE_JOINS = 4096;
+
+// A work item of the attention: pages lo .. hi - 1 of a row of the batch. Rows
+// in several pieces keep each piece's partial state in a slot.
+struct CacheItem {
+  int row, seq, start, count;   // row of the batch, its sequence, first new position and how many
+  int lo, hi;
+  int piece, pieces;            // this one of so many
+  int slot0;                    // slot of the row's first piece
+  int pad[3];
+};
 
 struct CacheDev {
   int L, H, KV, dh, bf16;
@@ -43,11 +53,10 @@ struct CacheDev {
   int32_t *list;      // [n_pages] scratch: pages in the order of a scan
   int32_t *map;       // [n_pages] scratch of copies: destination page
   uint32_t *mark;     // [ceil(n_pages / 32)] scratch of copies: pages to copy
-  int32_t *counts;    // [8] scratch: items of the plan, pages to copy
+  int32_t *counts;    // [8] items of the plan, pages to copy, a word of freeb before which no page is free
   // plan of the call in progress, one row per sequence of the batch
   int32_t *p_seq, *p_start, *p_count;   // [S]
-  int32_t *p_item;    // [S + 1] first item of each row
-  int4 *items;        // work items: row, first page, end page, slot of the partial state (-1: the row's one item)
+  CacheItem *items;
   int max_items;
   float *part;        // partial states of split rows
   int32_t *joins;     // [CACHE_JOINS] splits that have arrived; zero between calls

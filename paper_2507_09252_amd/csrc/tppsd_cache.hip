@@ -25,46 +25,50 @@ __device__ __forceinline__ void st_agent(int32_t *p, int v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// exclusive sum of v over the workgroup's threads in order; *total: the whole sum
-__device__ int block_scan(int v, int *total) {
-  __shared__ int sums[PLAN_NT / 64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
+struct Sums {
+  int a, b, top;   // two exclusive sums and a maximum
+};
+// over the workgroup's threads in order: *before the sums ahead of this thread,
+// returned the whole (and the largest top). `sums`: a slot per wave.
+__device__ Sums block_sums(Sums v, Sums *before, Sums *sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  Sums x = v;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
+    const int ya = __shfl_up(x.a, d, 64), yb = __shfl_up(x.b, d, 64), yt = __shfl_up(x.top, d, 64);
+    if (lane >= d) x.a += ya, x.b += yb, x.top = max(x.top, yt);
   }
   __syncthreads();   // (the last call's sums have been read)
   if (lane == 63) sums[wave] = x;
   __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < PLAN_NT / 64; ++w) {
-    const int s = sums[w];
-    before += w < wave ? s : 0;
-    all += s;
+  Sums ahead = {0, 0, 0}, all = {0, 0, 0};
+  for (int w = 0; w < waves; ++w) {
+    const Sums s = sums[w];
+    if (w < wave) ahead.a += s.a, ahead.b += s.b;
+    all.a += s.a, all.b += s.b, all.top = max(all.top, s.top);
   }
-  *total = all;
-  return before + x - v;
+  before->a = ahead.a + x.a - v.a;
+  before->b = ahead.b + x.b - v.b;
+  return all;
 }
 
-// The set bits of bits[0 .. nbits) in ascending order into list, until at least
+// The set bits of bits[0 .. nbits) in ascending order into list, from word w0 on, until at least
 // `want` are found; returns how many (at most want).
-__device__ int list_bits(const uint32_t *bits, int nbits, int want, int32_t *list) {
+__device__ int list_bits(const uint32_t *bits, int nbits, int w0, int want, int32_t *list, Sums *sums) {
   const int words = (nbits + 31) / 32;
   int found = 0;
-  for (int w0 = 0; w0 < words && found < want; w0 += PLAN_NT) {
+  for (; w0 < words && found < want; w0 += blockDim.x) {
     const int w = w0 + threadIdx.x;
     uint32_t m = w < words ? ld_agent(bits + w) : 0u;
-    int total;
-    int k = found + block_scan(__popc(m), &total);
+    Sums before;
+    const Sums all = block_sums(Sums{(int)__popc(m), 0, 0}, &before, sums);
+    int k = found + before.a;
     while (m && k < want) {
       const int bit = __ffs(m) - 1;
       m &= m - 1;
       list[k++] = w * 32 + bit;
     }
-    found += total;
+    found += all.a;
   }
   __syncthreads();   // the list is complete (one workgroup: its global writes are visible past the barrier)
   return min(found, want);
@@ -72,7 +76,10 @@ __device__ int list_bits(const uint32_t *bits, int nbits, int want, int32_t *lis
 
 // gives a page back: the last holder sets its bit
 __device__ __forceinline__ void page_drop(const CacheDev &c, int page) {
-  if (atomicSub(&c.refs[page], 1) == 1) atomicOr(&c.freeb[page >> 5], 1u << (page & 31));
+  if (atomicSub(&c.refs[page], 1) == 1) {
+    atomicOr(&c.freeb[page >> 5], 1u << (page & 31));
+    atomicMin(&c.counts[2], page >> 5);
+  }
 }
 
 __global__ void k_cache_reset(CacheDev c) {
@@ -86,17 +93,21 @@ __global__ void k_cache_reset(CacheDev c) {
     c.mark[j] = 0u;
   }
   for (size_t j = i; j < (size_t)CACHE_JOINS; j += n) c.joins[j] = 0;
-  if (i == 0) *c.status = 0u;
+  if (i == 0) {
+    *c.status = 0u;
+    c.counts[2] = 0;
+  }
 }
 
 // Plans a call: which sequence each row of the batch names, its first new
 // position and how many it brings; pages for the blocks that become whole; and
-// the work items of the split attention. One workgroup: the whole batch's
-// bookkeeping is a few thousand integers.
+// the attention's work items. One workgroup, as many threads as rows: the
+// batch's bookkeeping is a few integers a row, and two sums over the rows are
+// all that threads exchange.
 __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
-  __shared__ int tops[PLAN_NT / 64];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (b.B + PLAN_NT - 1) / PLAN_NT, i0 = min(b.B, tid * per), i1 = min(b.B, i0 + per);
+  __shared__ Sums sums[PLAN_NT / 64];
+  const int tid = threadIdx.x, nt = blockDim.x;
+  const int per = (b.B + nt - 1) / nt, i0 = min(b.B, tid * per), i1 = min(b.B, i0 + per);
   if (b.seqs) {
     // a sequence that is named twice belongs to the first row that names it
     for (int i = i0; i < i1; ++i) {
@@ -112,7 +123,10 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
     __threadfence();
     __syncthreads();
   }
-  int need_sum = 0;
+  auto top_of = [&](int start, int cnt) { return cnt > 0 ? (start + cnt - 1) / CACHE_BLOCK : 0; };
+  auto need_of = [&](int start, int cnt, int held) { return cnt > 0 ? max(0, (start + cnt) / CACHE_BLOCK - held) : 0; };
+  const int hint = c.counts[2];
+  Sums mine = {0, 0, 0}, before;
   for (int i = i0; i < i1; ++i) {
     int s = b.seqs ? b.seqs[i] : i;
     bool ok = s >= 0 && s < c.S;
@@ -120,6 +134,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
     if (!ok) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
     int start = 0, cnt = 0;
     if (ok) {
+      const int held = c.held[s];
       start = b.start_in ? b.start_in[i] + b.start_off : c.lens[s];
       cnt = b.counts ? min(max(b.counts[i], 0), b.P) : b.P;
       if (b.done && b.done[i]) cnt = 0;
@@ -128,22 +143,25 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
         if (cnt > 0) atomicOr(c.status, TPPSD_STATUS_CAPACITY);
         cnt = 0;
       }
-      need_sum += max(0, (cnt > 0 ? (start + cnt) / CACHE_BLOCK : 0) - c.held[s]);
+      mine.a += need_of(start, cnt, held);
     }
+    const int top = top_of(start, cnt);
+    mine.b += top;
+    mine.top = max(mine.top, top);
     c.p_seq[i] = ok ? s : -1;
     c.p_start[i] = start;
     c.p_count[i] = cnt;
   }
-  int total;
-  int off = block_scan(need_sum, &total);
-  const int avail = total > 0 ? list_bits(c.freeb, c.n_pages, total, c.list) : 0;
-  int pages_sum = 0, top_max = 0;
+  Sums all = block_sums(mine, &before, sums);
+  const int avail = all.a > 0 ? list_bits(c.freeb, c.n_pages, hint, all.a, c.list, sums) : 0;
+  int off = before.a;
+  mine.b = mine.top = 0;
   for (int i = i0; i < i1; ++i) {
     const int s = c.p_seq[i];
     if (s < 0) continue;
-    const int start = c.p_start[i];
+    const int start = c.p_start[i], held = c.held[s];
     int cnt = c.p_count[i];
-    const int held = c.held[s], need = max(0, (cnt > 0 ? (start + cnt) / CACHE_BLOCK : 0) - held);
+    const int need = need_of(start, cnt, held);
     if (need > 0) {
       if (off + need <= avail) {
         for (int j = 0; j < need; ++j) {
@@ -153,6 +171,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
           atomicAnd(&c.freeb[page >> 5], ~(1u << (page & 31)));
         }
         c.held[s] = held + need;
+        if (off + need == avail) c.counts[2] = c.list[avail - 1] >> 5;   // (no free page before the last one taken)
       } else {   // the rows before took the pages that were left
         atomicOr(c.status, TPPSD_STATUS_PAGES);
         c.p_count[i] = cnt = 0;
@@ -160,53 +179,48 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
       off += need;
     }
     c.pend[s] = cnt;
-    if (cnt > 0) {
-      const int top = (start + cnt - 1) / CACHE_BLOCK;
-      c.low[s] = max(top - 1, min(c.low[s], start / CACHE_BLOCK));
-      pages_sum += top;
-      top_max = max(top_max, top);
-    }
+    const int top = top_of(start, cnt);
+    if (cnt > 0) c.low[s] = max(top - 1, min(c.low[s], start / CACHE_BLOCK));
+    mine.b += top;
+    mine.top = max(mine.top, top);
   }
-  // Work items. Rows of about equal length that fill the chip are taken whole;
-  // otherwise pages are dealt out in pieces of a third of a workgroup's share.
-  // Pieces of the same row share one of the slots that their partial states take.
-  int all_pages;
-  block_scan(pages_sum, &all_pages);
-  if (lane == 0) tops[wave] = 0;
-  __syncthreads();
-  const int wave_top = (int)lanes_max((float)top_max);
-  if (lane == 0) tops[wave] = wave_top;
-  __syncthreads();
-  int most = 0;
-#pragma unroll
-  for (int w = 0; w < PLAN_NT / 64; ++w) most = max(most, tops[w]);
+  if (avail < all.a) all = block_sums(mine, &before, sums);   // (rows were left out)
+  // Work items. Rows of about equal length that fill the chip are taken whole.
+  // Otherwise pages are dealt out in pieces of a workgroup's share, or, where
+  // many rows leave many remainders, of a third of it. Pieces of a row have
+  // adjoining slots for their partial states.
   int chunk = INT32_MAX;
   if (b.split_target > 0) {
-    const int share = (all_pages + b.split_target - 1) / b.split_target;
-    if (most > share + share / 4) chunk = max(CACHE_MIN_PIECE, (all_pages + 3 * b.split_target - 1) / (3 * b.split_target));
+    const int share = (all.b + b.split_target - 1) / b.split_target, parts = b.B * 4 <= b.split_target ? 1 : 3;
+    if (all.top > share + share / 4)
+      chunk = max(CACHE_MIN_PIECE, (all.b + parts * b.split_target - 1) / (parts * b.split_target));
   }
-  auto splits = [&](int i) {
-    const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0;
-    return top <= chunk ? 1 : (top + chunk - 1) / chunk;
-  };
-  int item_sum = 0, slot_sum = 0;
+  auto pieces = [&](int top) { return top <= chunk ? 1 : (top + chunk - 1) / chunk; };
+  mine = {0, 0, 0};
   for (int i = i0; i < i1; ++i) {
-    const int n = splits(i);
-    item_sum += n;
-    slot_sum += n > 1 ? n : 0;
+    const int n = pieces(top_of(c.p_start[i], c.p_count[i]));
+    mine.a += n;
+    mine.b += n > 1 ? n : 0;
   }
-  int n_items, n_slots;
-  int at = block_scan(item_sum, &n_items), slot = block_scan(slot_sum, &n_slots);
+  all = block_sums(mine, &before, sums);
   for (int i = i0; i < i1; ++i) {
-    const int cnt = c.p_count[i], top = cnt > 0 ? (c.p_start[i] + cnt - 1) / CACHE_BLOCK : 0, n = splits(i);
-    c.p_item[i] = at;
-    for (int j = 0; j < n; ++j)
-      c.items[at++] = n == 1 ? make_int4(i, 0, top, -1) : make_int4(i, j * chunk, min(top, (j + 1) * chunk), slot++);
+    CacheItem it;
+    it.row = i;
+    it.seq = c.p_seq[i];
+    it.start = c.p_start[i];
+    it.count = c.p_count[i];
+    const int top = top_of(it.start, it.count);
+    it.pieces = pieces(top);
+    it.slot0 = before.b;
+    it.lo = 0;
+    for (it.piece = 0; it.piece < it.pieces; ++it.piece) {
+      it.hi = it.piece + 1 == it.pieces ? top : it.lo + chunk;
+      c.items[before.a++] = it;
+      it.lo = it.hi;
+    }
+    if (it.pieces > 1) before.b += it.pieces;
   }
-  if (tid == 0) {
-    c.p_item[b.B] = n_items;
-    c.counts[0] = n_items;
-  }
+  if (tid == 0) c.counts[0] = all.a;
 }
 
 __global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
@@ -354,8 +368,9 @@ __global__ void k_copy_mark(CacheDev to, CacheDev from, const int32_t *src, cons
 
 // the marked pages in ascending order get the destination's lowest free pages
 __global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev from) {
-  const int n = list_bits(from.mark, from.n_pages, from.n_pages, from.list);
-  const int avail = n > 0 ? list_bits(to.freeb, to.n_pages, n, to.list) : 0;
+  __shared__ Sums sums[PLAN_NT / 64];
+  const int n = list_bits(from.mark, from.n_pages, 0, from.n_pages, from.list, sums);
+  const int avail = n > 0 ? list_bits(to.freeb, to.n_pages, to.counts[2], n, to.list, sums) : 0;
   const bool fits = avail == n;
   for (int k = threadIdx.x; k < n && fits; k += PLAN_NT) {
     const int page = to.list[k];
@@ -365,6 +380,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev fro
   }
   if (threadIdx.x == 0) {
     to.counts[1] = fits ? n : -1;
+    if (fits && n > 0) to.counts[2] = to.list[n - 1] >> 5;
     if (!fits) atomicOr(to.status, TPPSD_STATUS_PAGES);
   }
 }
@@ -573,7 +589,7 @@ void launch_cache_reset(const CacheDev &c, hipStream_t st) {
 }
 
 void launch_cache_begin(const CacheDev &c, const CacheBegin &b, hipStream_t st) {
-  k_cache_begin<<<1, PLAN_NT, 0, st>>>(c, b);
+  k_cache_begin<<<1, std::min(PLAN_NT, (b.B + 63) / 64 * 64), 0, st>>>(c, b);
 }
 
 void launch_cache_append(const CacheDev &c, int layer, int B, int P, const CacheRows &r, hipStream_t st) {

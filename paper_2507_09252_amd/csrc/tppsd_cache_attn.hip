@@ -29,6 +29,7 @@ namespace tppsd {
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int EIGHT_PAGES = 32;   // pages of a sequence at its longest from which eight waves share it
 
 // 8 values as bf16 operands: one part for bf16 sources; for fp32 three parts
 // that add up to the value (each the bf16 rounding of what the ones before
@@ -70,21 +71,28 @@ __device__ __forceinline__ f32x4_t mma(short4_t a, short4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
 
-// 8 elements between memory (16-byte aligned) and registers
-template <typename ACT> __device__ __forceinline__ void load8(ACT (&x)[8], const ACT *p) {
-  constexpr int W = sizeof(ACT) * 8 / 16;
-  uint4 w[W];
+// 8 elements in registers as 16-byte words (two for fp32), and element e of them
+template <typename ACT> struct Eight {
+  static constexpr int W = sizeof(ACT) * 8 / 16;
+  u32x4_t w[W];
+  __device__ __forceinline__ void load(const ACT *p) {
 #pragma unroll
-  for (int i = 0; i < W; ++i) w[i] = ((const uint4 *)p)[i];
-  __builtin_memcpy(x, w, sizeof x);
-}
-template <typename ACT> __device__ __forceinline__ void store8(ACT *p, const ACT (&x)[8]) {
-  constexpr int W = sizeof(ACT) * 8 / 16;
-  uint4 w[W];
-  __builtin_memcpy(w, x, sizeof x);
+    for (int i = 0; i < W; ++i) w[i] = ((const u32x4_t *)p)[i];
+  }
+  __device__ __forceinline__ void store(ACT *p) const {
 #pragma unroll
-  for (int i = 0; i < W; ++i) ((uint4 *)p)[i] = w[i];
-}
+    for (int i = 0; i < W; ++i) ((u32x4_t *)p)[i] = w[i];
+  }
+  __device__ __forceinline__ ACT at(int e) const {
+    if constexpr (W == 1) return (ACT)(w[0][e >> 1] >> (16 * (e & 1)));
+    else return __uint_as_float(w[e >> 2][e & 3]);
+  }
+  // (e even first: a bf16 word is put together from its two elements)
+  __device__ __forceinline__ void put(int e, ACT v) {
+    if constexpr (W == 1) w[0][e >> 1] = e & 1 ? w[0][e >> 1] | (uint32_t)v << 16 : (uint32_t)v;
+    else w[e >> 2][e & 3] = __float_as_uint(v);
+  }
+};
 
 // the operand of a query or key row at p (8 elements, 4 for d_head 16), part by part into to(part)
 template <typename ACT, int DH, typename TO> __device__ __forceinline__ void load_k(const ACT *p, TO to) {
@@ -358,9 +366,8 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, rr = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, G = c.H / c.KV, item = blockIdx.x;
   if (item >= c.counts[0]) return;
-  const int4 it = c.items[item];
-  const int i = it.x, slot = it.w;   // slot of this split's partial state, -1: the row's one item
-  const int cnt = c.p_count[i], start = c.p_start[i], seq = c.p_seq[i];
+  const CacheItem it = c.items[item];
+  const int i = it.row, cnt = it.count, start = it.start, seq = it.seq;
   const size_t head0 = (size_t)h * G * DH;
   ACT *const O = (ACT *)a.o;
   // this group: query heads hd0 .. + hn - 1 of positions p0 .. + pn - 1
@@ -384,10 +391,10 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
   if (pn <= 0) return;   // (the group's position range of this row is empty: for all its splits)
   const int end = start + cnt;
   const int ba = p0 / CACHE_BLOCK, bb = (p0 + pn - 1) / CACHE_BLOCK;
-  const bool tail = it.z >= (end - 1) / CACHE_BLOCK;
+  const bool tail = it.piece + 1 == it.pieces;
   // the split that takes the group's own block: the one whose pages it is among,
   // or would follow
-  const bool mine = ONE ? tail : (it.y <= ba && ba < it.z) || (tail && ba >= it.z);
+  const bool mine = ONE ? tail : (it.lo <= ba && ba < it.hi) || (tail && ba >= it.hi);
   R s;
   s.g = g;
   s.scale2 = a.scale * LOG2E;
@@ -409,7 +416,7 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
   // ---- rows of the queries' own blocks, into LDS (and the cache) ------------
   const size_t layer0 = (size_t)a.layer * c.n_pages;
   const int32_t *table = c.table + (size_t)seq * c.NP;
-  const int j0 = it.y, j1 = min(it.z, ba);
+  const int j0 = it.lo, j1 = min(it.hi, ba);
   auto tile_of = [&](int page) { return (layer0 + page) * c.KV + h; };
   auto load_side = [&](uint4 (&w)[NU], size_t tile, int side) {
     const uint4 *p = (const uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)) + side * (64 * NU) + lane;
@@ -449,25 +456,26 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
         vp = (const ACT *)src.v + i * src.v_sb + h * src.v_sh +
              (blocked ? (size_t)(pr >> 3) * 8 * DH + j * 8 + (pr & 7) : (size_t)pr * src.v_sp + j);
       }
-      ACT kk[8], vv[8];
+      Eight<ACT> kk, vv;
       const bool in = row < n;
-      load8(kk, kp);
+      kk.load(kp);
       if (blocked) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) vv[e] = vp[8 * e];
+        for (int e = 0; e < 8; ++e) vv.put(e, vp[8 * e]);
       } else {
-        load8(vv, vp);
+        vv.load(vp);
       }
-      store8(&win.k[row][j], kk);
+      kk.store(&win.k[row][j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        win.v[j + e][row] = in ? vv[e] : (ACT)0;
-        bad |= in && not_finite(ld(&vv[e], 0));
+        const ACT v = in ? vv.at(e) : (ACT)0;
+        win.v[j + e][row] = v;
+        bad |= not_finite(ld(&v, 0));
       }
       if (ONE && in && pos >= start) {
         ACT *to = (ACT *)ring + (pos % CACHE_RING) * DH + j;
-        store8(to, kk);
-        store8(to + CACHE_RING * DH, vv);
+        kk.store(to);
+        vv.store(to + CACHE_RING * DH);
       }
     }
     any_bad = __syncthreads_or(bad);
@@ -579,46 +587,60 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
   // ---- sums over the lane groups, then over the waves ----------------------
 #pragma unroll
   for (int t = 0; t < MT; ++t) s.l[t] = NP == 1 ? s.l1[t][0] : xor32_sum(xor16_sum(s.l[t]));
+  // wave 0 gets the state of all waves
+  auto fold_waves = [&] {
 #pragma unroll
-  for (int half = NW / 2; half > 0; half >>= 1) {
-    if (wave >= half && wave < 2 * half) {
+    for (int half = NW / 2; half > 0; half >>= 1) {
+      if (wave >= half && wave < 2 * half) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          fold.m[wave - half][t][lane] = s.m[t];
+          fold.l[wave - half][t][lane] = s.l[t];
+#pragma unroll
+          for (int u = 0; u < NU; ++u) fold.o[wave - half][t * NU + u][lane] = s.o[t][u];
+        }
+      }
+      __syncthreads();
+      if (wave < half)
+        s.fold([&](int t) { return fold.m[wave][t][lane]; }, [&](int t) { return fold.l[wave][t][lane]; },
+               [&](int t, int u) { return fold.o[wave][t * NU + u][lane]; });
+      if (half > 1) __syncthreads();
+    }
+  };
+  fold_waves();
+  if (it.pieces > 1) {
+    // [slot][head][group][o, m, l][64]: lane by lane. The state goes out and comes
+    // in by accesses that are coherent over the whole GPU (its dies have an L2
+    // each), so that no cache has to be written back (with fences at that scope
+    // instead, 48 ragged rows took 153 us, not 83): the wait puts the stores ahead
+    // of the arrival.
+    constexpr int N = 4 * MT * NU + 2 * MT;
+    const int Z = gridDim.z;
+    auto part = [&](int piece) { return c.part + (((size_t)(it.slot0 + piece) * c.KV + h) * Z + z) * N * 64 + lane; };
+    int *arrived = c.joins + ((size_t)i * c.KV + h) * Z + z;
+    if (wave == 0) {
+      float *pp = part(it.piece);
+      auto put = [&](int at, float v) { __hip_atomic_store(pp + 64 * at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        fold.m[wave - half][t][lane] = s.m[t];
-        fold.l[wave - half][t][lane] = s.l[t];
 #pragma unroll
-        for (int u = 0; u < NU; ++u) fold.o[wave - half][t * NU + u][lane] = s.o[t][u];
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) put(4 * (t * NU + u) + e, s.o[t][u][e]);
+        put(4 * MT * NU + t, s.m[t]);
+        put(4 * MT * NU + MT + t, s.l[t]);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (lane == 0) {
+        const int before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last_of_row = before == it.pieces - 1;
+        if (before == it.pieces - 1) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
     __syncthreads();
-    if (wave < half)
-      s.fold([&](int t) { return fold.m[wave][t][lane]; }, [&](int t) { return fold.l[wave][t][lane]; },
-             [&](int t, int u) { return fold.o[wave][t * NU + u][lane]; });
-    if (half > 1) __syncthreads();
-  }
-  if (wave != 0) return;
-  if (slot >= 0) {
-    // [slot][head][group][o, m, l][64]: lane by lane
-    constexpr int N = 4 * MT * NU + 2 * MT;
-    const int Z = gridDim.z, it0 = c.p_item[i], ns = c.p_item[i + 1] - it0, s0 = slot - (item - it0);
-    auto part = [&](int sl) { return c.part + (((size_t)sl * c.KV + h) * Z + z) * N * 64; };
-    float *pp = part(slot);
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-#pragma unroll
-      for (int u = 0; u < NU; ++u) ((f32x4_t *)pp)[64 * (t * NU + u) + lane] = s.o[t][u];
-      pp[64 * (4 * MT * NU + t) + lane] = s.m[t];
-      pp[64 * (4 * MT * NU + MT + t) + lane] = s.l[t];
-    }
-    __threadfence();
-    int *arrived = c.joins + ((size_t)i * c.KV + h) * Z + z;
-    int before = 0;
-    if (lane == 0) before = __hip_atomic_fetch_add(arrived, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-    before = __builtin_amdgcn_readfirstlane(before);
-    if (before != ns - 1) return;
-    __threadfence();
-    if (lane == 0) __hip_atomic_store(arrived, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // the splits in order, whoever comes last
+    if (!last_of_row) return;
+    asm volatile("" ::: "memory");
+    // the pieces, dealt to the waves in order whoever comes last
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       s.m[t] = -INFINITY;
@@ -626,13 +648,18 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
 #pragma unroll
       for (int u = 0; u < NU; ++u) s.o[t][u] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
-    for (int x = 0; x < ns; ++x) {
-      const float *pq = part(s0 + x);
-      s.fold([&](int t) { return pq[64 * (4 * MT * NU + t) + lane]; },
-             [&](int t) { return pq[64 * (4 * MT * NU + MT + t) + lane]; },
-             [&](int t, int u) { return ((const f32x4_t *)pq)[64 * (t * NU + u) + lane]; });
+    for (int x = wave; x < it.pieces; x += NW) {
+      const float *pq = part(x);
+      auto get = [&](int at) { return __hip_atomic_load(pq + 64 * at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+      s.fold([&](int t) { return get(4 * MT * NU + t); }, [&](int t) { return get(4 * MT * NU + MT + t); },
+             [&](int t, int u) {
+               const int at = 4 * (t * NU + u);
+               return (f32x4_t){get(at), get(at + 1), get(at + 2), get(at + 3)};
+             });
     }
+    fold_waves();
   }
+  if (wave != 0) return;
   // ---- normalise and store: lane (rr, g) holds columns 16 u + 4 g .. + 3 of query rr ----
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
@@ -674,29 +701,40 @@ int call_groups(const CacheDev &c, int P) {
   return groups_of(G, 16 * (one ? tiles_of(c, (long)P * G) : max_tiles(c.dh, c.bf16)), P, one);
 }
 
+// Waves of a workgroup: eight where their registers and LDS leave room and
+// either sequences may be long or there are too few workgroups for the chip
+// anyway; four otherwise.
+constexpr bool eight_fit(int dh, bool bf16, int mt, bool one) { return one && dh <= (bf16 ? 64 : 32) && mt < 4; }
+int waves_of(const CacheDev &c, int B, int P) {
+  const bool one = one_group(c, P);
+  if (!eight_fit(c.dh, c.bf16, tiles_of(c, (long)P * (c.H / c.KV)), one)) return 4;
+  return c.NP >= EIGHT_PAGES || (long)B * c.KV <= 256 ? 8 : 4;
+}
+
 }  // namespace
 
 int cache_split_target(const CacheDev &c, int B, int P) {
-  const long per = (long)c.KV * call_groups(c, P);
-  return per > CACHE_SPLIT_WGS || B * per > CACHE_JOINS ? 0 : (int)(CACHE_SPLIT_WGS / per);
+  const long per = (long)c.KV * call_groups(c, P), full = CACHE_SPLIT_WAVES / waves_of(c, B, P);
+  return per > full || B * per > CACHE_JOINS ? 0 : (int)(full / per);
 }
 
 // a row, and for a split batch about three times the target more
-int cache_max_items(int S, int KV) { return S + 3 * (CACHE_SPLIT_WGS / KV + 1) + 2; }
+int cache_max_items(int S, int KV) { return S + 3 * (CACHE_SPLIT_WAVES / 4 / KV + 1) + 2; }
 
 // Partial states: a row of t pages in pieces of C >= pages / (3 target) takes
 // ceil(t / C) < 2 t / C slots, so all rows at most 6 target, each of heads x
-// groups states; target x heads x groups <= CACHE_SPLIT_WGS. A state is
+// groups states; target x heads x groups <= CACHE_SPLIT_WAVES / 4. A state is
 // output, maximum and sum of up to four tiles of 16 query rows, lane by lane.
 size_t cache_part_floats(const CacheDev &c) {
   const size_t groups = (size_t)call_groups(c, c.max_events);
   const size_t few = c.KV * groups * ((size_t)c.S + (size_t)c.S * c.NP / CACHE_MIN_PIECE);
-  return std::min<size_t>(6 * CACHE_SPLIT_WGS, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
+  return std::min<size_t>(6 * CACHE_SPLIT_WAVES / 4, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
 }
 
 void launch_cache_attend(const CacheDev &c, const CacheAttend &a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
   const long R = (long)a.P * (c.H / c.KV);
   const bool one = one_group(c, a.P);
+  const int waves = waves_of(c, a.B, a.P);
   const int target = cache_split_target(c, a.B, a.P), items = a.B + (target ? 3 * target + 1 : 0);
   if (!one) launch_cache_append(c, a.layer, a.B, a.P, a.kv, st);
   auto go = [&](auto act, auto width) {
@@ -705,9 +743,14 @@ void launch_cache_attend(const CacheDev &c, const CacheAttend &a, hipStream_t st
     auto launch = [&](auto mt, auto is_one) {
       constexpr int MT = decltype(mt)::value;
       constexpr bool ONE = decltype(is_one)::value;
-      constexpr int NW = ONE && DH * (int)sizeof(ACT) <= 128 && MT < 4 ? 8 : 4;
-      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, NW, ONE>), dim3(items, c.KV, call_groups(c, a.P)), dim3(64 * NW),
-                            0, st, ev0, ev1, 0, c, a);
+      const dim3 grid(items, c.KV, call_groups(c, a.P));
+      if constexpr (eight_fit(DH, sizeof(ACT) == 2, MT, ONE)) {
+        if (waves == 8) {
+          hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 8, ONE>), grid, dim3(512), 0, st, ev0, ev1, 0, c, a);
+          return;
+        }
+      }
+      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 4, ONE>), grid, dim3(256), 0, st, ev0, ev1, 0, c, a);
     };
     constexpr int MOST = max_tiles(DH, sizeof(ACT) == 2);
     const int mt = tiles_of(c, R);
