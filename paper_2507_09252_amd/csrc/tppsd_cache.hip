@@ -6,6 +6,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "../../include/tppsd.h"
 #include "tppsd_cache_device.h"
 
@@ -21,35 +24,53 @@ __device__ __forceinline__ int ld_agent(const int32_t *p) {
 __device__ __forceinline__ uint32_t ld_agent(const uint32_t *p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+// a barrier behind which the workgroup's accesses to the L2 (atomics, and the loads and stores here) are done
+__device__ __forceinline__ void sync_agent() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
 __device__ __forceinline__ void st_agent(int32_t *p, int v) {
   __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// running sum over the wave's lanes, this one included (row shifts, then row and half-wave broadcasts)
+__device__ __forceinline__ int wave_scan(int v) {
+  auto add = [&](auto ctrl, auto rows) {
+    v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xF, false);
+  };
+  add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xF>{});   // row_shr:1, 2, 4, 8
+  add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xF>{});
+  add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xF>{});
+  add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xF>{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xA>{});   // row_bcast:15
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xC>{});   // row_bcast:31
+  return v;
+}
+
 struct Sums {
-  int a, b, top;   // two exclusive sums and a maximum
+  int a, b, top;   // two exclusive sums and a maximum (of numbers below 2^24, exact as floats)
 };
 // over the workgroup's threads in order: *before the sums ahead of this thread,
 // returned the whole (and the largest top). `sums`: a slot per wave.
 __device__ Sums block_sums(Sums v, Sums *before, Sums *sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  Sums x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int ya = __shfl_up(x.a, d, 64), yb = __shfl_up(x.b, d, 64), yt = __shfl_up(x.top, d, 64);
-    if (lane >= d) x.a += ya, x.b += yb, x.top = max(x.top, yt);
+  const Sums x = {wave_scan(v.a), wave_scan(v.b), (int)lanes_max((float)v.top)};
+  if (waves == 1) {
+    before->a = x.a - v.a;
+    before->b = x.b - v.b;
+    return {__builtin_amdgcn_readlane(x.a, 63), __builtin_amdgcn_readlane(x.b, 63), x.top};
   }
   __syncthreads();   // (the last call's sums have been read)
   if (lane == 63) sums[wave] = x;
   __syncthreads();
-  Sums ahead = {0, 0, 0}, all = {0, 0, 0};
-  for (int w = 0; w < waves; ++w) {
-    const Sums s = sums[w];
-    if (w < wave) ahead.a += s.a, ahead.b += s.b;
-    all.a += s.a, all.b += s.b, all.top = max(all.top, s.top);
-  }
-  before->a = ahead.a + x.a - v.a;
-  before->b = ahead.b + x.b - v.b;
-  return all;
+  // lane w has the sums of wave w
+  const Sums mine = lane < waves ? sums[lane] : Sums{0, 0, 0};
+  const int ra = wave_scan(mine.a), rb = wave_scan(mine.b);
+  const int last = waves - 1, prev = max(wave - 1, 0);
+  const int ua = __builtin_amdgcn_readfirstlane(__shfl(ra, prev, 64)), ub = __builtin_amdgcn_readfirstlane(__shfl(rb, prev, 64));
+  before->a = (wave ? ua : 0) + x.a - v.a;
+  before->b = (wave ? ub : 0) + x.b - v.b;
+  return {__shfl(ra, last, 64), __shfl(rb, last, 64), (int)lanes_max((float)mine.top)};
 }
 
 // The set bits of bits[0 .. nbits) in ascending order into list, from word w0 on, until at least
@@ -74,12 +95,23 @@ __device__ int list_bits(const uint32_t *bits, int nbits, int w0, int want, int3
   return min(found, want);
 }
 
-// gives a page back: the last holder sets its bit
-__device__ __forceinline__ void page_drop(const CacheDev &c, int page) {
-  if (atomicSub(&c.refs[page], 1) == 1) {
-    atomicOr(&c.freeb[page >> 5], 1u << (page & 31));
-    atomicMin(&c.counts[2], page >> 5);
+// gives pages [j0, j1) of a sequence's table back, a workgroup's threads
+// together: the last holder sets a page's bit. counts[2], where the search for
+// free pages begins, is one address for the whole chip: it is read first, and
+// as it only falls here, hardly any thread has to write it.
+__device__ __forceinline__ void pages_drop(const CacheDev &c, int s, int j0, int j1) {
+  const int seen = c.counts[2];
+  int low = INT32_MAX;
+  for (int j = j0 + threadIdx.x; j < j1; j += blockDim.x) {
+    int32_t *e = &c.table[(size_t)s * c.NP + j];
+    const int page = *e;
+    *e = -1;
+    if (atomicSub(&c.refs[page], 1) == 1) {
+      atomicOr(&c.freeb[page >> 5], 1u << (page & 31));
+      low = min(low, page >> 5);
+    }
   }
+  if (low < seen) atomicMin(&c.counts[2], low);
 }
 
 __global__ void k_cache_reset(CacheDev c) {
@@ -101,89 +133,106 @@ __global__ void k_cache_reset(CacheDev c) {
 
 // Plans a call: which sequence each row of the batch names, its first new
 // position and how many it brings; pages for the blocks that become whole; and
-// the attention's work items. One workgroup, as many threads as rows: the
-// batch's bookkeeping is a few integers a row, and two sums over the rows are
-// all that threads exchange.
-__global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
+// the attention's work items. One workgroup, as many threads as rows (PER rows
+// a thread past 1024, held in registers; 0: any number, in memory): the batch's
+// bookkeeping is a few integers a row, and two sums over the rows are all that
+// threads exchange. 64 rows 3.7 us, 4096 rows MEASURE.
+template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
   __shared__ Sums sums[PLAN_NT / 64];
   const int tid = threadIdx.x, nt = blockDim.x;
-  const int per = (b.B + nt - 1) / nt, i0 = min(b.B, tid * per), i1 = min(b.B, i0 + per);
+  const int per = PER ? PER : (b.B + nt - 1) / nt, i0 = min(b.B, tid * per), n = min(b.B, i0 + per) - i0;
+  struct Row {
+    int seq, start, cnt, held;
+  };
+  Row mem[PER ? PER : 1];
+  // f(i, row of the batch, its plan): the plan stays between passes
+  auto each = [&](bool first, auto f) {
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int k = 0; k < PER; ++k)
+        if (k < n) f(i0 + k, mem[k]);
+    } else {
+      for (int k = 0; k < n; ++k) {
+        const int i = i0 + k;
+        Row r;
+        if (!first) {
+          r.seq = c.p_seq[i], r.start = c.p_start[i], r.cnt = c.p_count[i];
+          r.held = r.seq >= 0 ? c.held[r.seq] : 0;
+        }
+        f(i, r);
+        c.p_seq[i] = r.seq, c.p_start[i] = r.start, c.p_count[i] = r.cnt;
+      }
+    }
+  };
   if (b.seqs) {
     // a sequence that is named twice belongs to the first row that names it
-    for (int i = i0; i < i1; ++i) {
-      const int s = b.seqs[i];
+    for (int k = 0; k < n; ++k) {
+      const int s = b.seqs[i0 + k];
       if (s >= 0 && s < c.S) st_agent(&c.owner[s], INT32_MAX);
     }
-    __threadfence();
-    __syncthreads();
-    for (int i = i0; i < i1; ++i) {
-      const int s = b.seqs[i];
-      if (s >= 0 && s < c.S) atomicMin(&c.owner[s], i);
+    sync_agent();
+    for (int k = 0; k < n; ++k) {
+      const int s = b.seqs[i0 + k];
+      if (s >= 0 && s < c.S) atomicMin(&c.owner[s], i0 + k);
     }
-    __threadfence();
-    __syncthreads();
+    sync_agent();
   }
-  auto top_of = [&](int start, int cnt) { return cnt > 0 ? (start + cnt - 1) / CACHE_BLOCK : 0; };
-  auto need_of = [&](int start, int cnt, int held) { return cnt > 0 ? max(0, (start + cnt) / CACHE_BLOCK - held) : 0; };
+  auto top_of = [&](const Row &r) { return r.cnt > 0 ? (r.start + r.cnt - 1) / CACHE_BLOCK : 0; };
+  auto need_of = [&](const Row &r) { return r.cnt > 0 ? max(0, (r.start + r.cnt) / CACHE_BLOCK - r.held) : 0; };
   const int hint = c.counts[2];
   Sums mine = {0, 0, 0}, before;
-  for (int i = i0; i < i1; ++i) {
-    int s = b.seqs ? b.seqs[i] : i;
+  each(true, [&](int i, Row &r) {
+    const int s = b.seqs ? b.seqs[i] : i;
     bool ok = s >= 0 && s < c.S;
     if (ok && b.seqs) ok = ld_agent(&c.owner[s]) == i;
-    if (!ok) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
-    int start = 0, cnt = 0;
+    r = {ok ? s : -1, 0, 0, 0};
     if (ok) {
-      const int held = c.held[s];
-      start = b.start_in ? b.start_in[i] + b.start_off : c.lens[s];
-      cnt = b.counts ? min(max(b.counts[i], 0), b.P) : b.P;
-      if (b.done && b.done[i]) cnt = 0;
-      else if (b.start_in) c.lens[s] = start;
-      if (start < 0 || cnt > c.max_events - start) {
-        if (cnt > 0) atomicOr(c.status, TPPSD_STATUS_CAPACITY);
-        cnt = 0;
+      const int want = b.counts ? b.counts[i] : b.P, done = b.done ? b.done[i] : 0;
+      r.held = c.held[s];
+      r.start = b.start_in ? b.start_in[i] + b.start_off : c.lens[s];
+      r.cnt = done ? 0 : min(max(want, 0), b.P);
+      if (b.start_in && !done) c.lens[s] = r.start;
+      if (r.start < 0 || r.cnt > c.max_events - r.start) {
+        if (r.cnt > 0) atomicOr(c.status, TPPSD_STATUS_CAPACITY);
+        r.cnt = 0;
       }
-      mine.a += need_of(start, cnt, held);
+    } else {
+      atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
     }
-    const int top = top_of(start, cnt);
-    mine.b += top;
-    mine.top = max(mine.top, top);
-    c.p_seq[i] = ok ? s : -1;
-    c.p_start[i] = start;
-    c.p_count[i] = cnt;
-  }
+    mine.a += need_of(r);
+    mine.b += top_of(r);
+    mine.top = max(mine.top, top_of(r));
+  });
   Sums all = block_sums(mine, &before, sums);
   const int avail = all.a > 0 ? list_bits(c.freeb, c.n_pages, hint, all.a, c.list, sums) : 0;
   int off = before.a;
   mine.b = mine.top = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int s = c.p_seq[i];
-    if (s < 0) continue;
-    const int start = c.p_start[i], held = c.held[s];
-    int cnt = c.p_count[i];
-    const int need = need_of(start, cnt, held);
-    if (need > 0) {
-      if (off + need <= avail) {
-        for (int j = 0; j < need; ++j) {
-          const int page = c.list[off + j];
-          c.table[(size_t)s * c.NP + held + j] = page;
-          c.refs[page] = 1;
-          atomicAnd(&c.freeb[page >> 5], ~(1u << (page & 31)));
+  each(false, [&](int i, Row &r) {
+    if (r.seq >= 0) {
+      const int need = need_of(r);
+      if (need > 0) {
+        if (off + need <= avail) {
+          for (int j = 0; j < need; ++j) {
+            const int page = c.list[off + j];
+            c.table[(size_t)r.seq * c.NP + r.held + j] = page;
+            c.refs[page] = 1;
+            atomicAnd(&c.freeb[page >> 5], ~(1u << (page & 31)));
+          }
+          c.held[r.seq] = r.held + need;
+          if (off + need == avail) c.counts[2] = c.list[avail - 1] >> 5;   // (no free page before the last one taken)
+        } else {   // the rows before took the pages that were left
+          atomicOr(c.status, TPPSD_STATUS_PAGES);
+          r.cnt = 0;
         }
-        c.held[s] = held + need;
-        if (off + need == avail) c.counts[2] = c.list[avail - 1] >> 5;   // (no free page before the last one taken)
-      } else {   // the rows before took the pages that were left
-        atomicOr(c.status, TPPSD_STATUS_PAGES);
-        c.p_count[i] = cnt = 0;
+        off += need;
       }
-      off += need;
+      c.pend[r.seq] = r.cnt;
+      if (r.cnt > 0) c.low[r.seq] = max(top_of(r) - 1, min(c.low[r.seq], r.start / CACHE_BLOCK));
     }
-    c.pend[s] = cnt;
-    const int top = top_of(start, cnt);
-    if (cnt > 0) c.low[s] = max(top - 1, min(c.low[s], start / CACHE_BLOCK));
-    mine.b += top;
-    mine.top = max(mine.top, top);
-  }
+    if (PER > 0) c.p_seq[i] = r.seq, c.p_start[i] = r.start, c.p_count[i] = r.cnt;
+    mine.b += top_of(r);
+    mine.top = max(mine.top, top_of(r));
+  });
   if (avail < all.a) all = block_sums(mine, &before, sums);   // (rows were left out)
   // Work items. Rows of about equal length that fill the chip are taken whole.
   // Otherwise pages are dealt out in pieces of a workgroup's share, or, where
@@ -197,19 +246,19 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
   }
   auto pieces = [&](int top) { return top <= chunk ? 1 : (top + chunk - 1) / chunk; };
   mine = {0, 0, 0};
-  for (int i = i0; i < i1; ++i) {
-    const int n = pieces(top_of(c.p_start[i], c.p_count[i]));
-    mine.a += n;
-    mine.b += n > 1 ? n : 0;
-  }
+  each(false, [&](int, Row &r) {
+    const int k = pieces(top_of(r));
+    mine.a += k;
+    mine.b += k > 1 ? k : 0;
+  });
   all = block_sums(mine, &before, sums);
-  for (int i = i0; i < i1; ++i) {
+  each(false, [&](int i, Row &r) {
     CacheItem it;
     it.row = i;
-    it.seq = c.p_seq[i];
-    it.start = c.p_start[i];
-    it.count = c.p_count[i];
-    const int top = top_of(it.start, it.count);
+    it.seq = r.seq;
+    it.start = r.start;
+    it.count = r.cnt;
+    const int top = top_of(r);
     it.pieces = pieces(top);
     it.slot0 = before.b;
     it.lo = 0;
@@ -219,7 +268,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin 
       it.lo = it.hi;
     }
     if (it.pieces > 1) before.b += it.pieces;
-  }
+  });
   if (tid == 0) c.counts[0] = all.a;
 }
 
@@ -262,17 +311,31 @@ __global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t 
     }
   }
   __syncthreads();
-  for (int j = range[0] + threadIdx.x; j < range[1]; j += blockDim.x) {
-    int32_t *e = &c.table[(size_t)s * c.NP + j];
-    page_drop(c, *e);
-    *e = -1;
-  }
+  pages_drop(c, s, range[0], range[1]);
 }
 
-// Which pairs of a fork or copy are carried out: both sequences exist, a
-// destination is named once (the first pair counts) and, within one cache, is
-// no pair's source. A pair of two negative numbers is none. Verdicts into
-// to.p_seq.
+// Whether pair i of a fork or copy is carried out: both sequences exist, no pair
+// before it names its destination and, within one cache, none as its source. A
+// pair of two negative numbers is none. Every workgroup looks through the whole
+// list for the pair it is about (few pairs; their verdicts depend on the list alone).
+__device__ bool pair_stands(const CacheDev &to, const CacheDev &from, int n, const int32_t *src, const int32_t *dst,
+                            int i, bool same) {
+  const int s = src[i], d = dst[i];
+  bool bad = s < 0 || s >= from.S || d < 0 || d >= to.S;
+  const bool none = s < 0 && d < 0;
+  if (!bad) {
+    for (int j = threadIdx.x; j < n; j += blockDim.x) {
+      const int sj = src[j], dj = dst[j];
+      if (sj < 0 || sj >= from.S || dj < 0 || dj >= to.S) continue;
+      bad |= (dj == d && j < i) || (same && sj == d);
+    }
+    bad = __syncthreads_or(bad);
+  }
+  if (bad && !none && threadIdx.x == 0) atomicOr(to.status, TPPSD_STATUS_SEQUENCE);
+  return !bad;
+}
+// The same for long lists, once for all pairs, into to.p_seq
+constexpr int FEW_PAIRS = 256;
 __global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev from, int n, const int32_t *src,
                                                          const int32_t *dst, int same) {
   auto ok = [&](int i) { return src[i] >= 0 && src[i] < from.S && dst[i] >= 0 && dst[i] < to.S; };
@@ -284,61 +347,58 @@ __global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev f
         st_agent(&to.role[src[i]], 0);
       }
     }
-  for (int w = threadIdx.x; w < (from.n_pages + 31) / 32 && !same; w += PLAN_NT) from.mark[w] = 0u;
-  __threadfence();
-  __syncthreads();
+  sync_agent();
   for (int i = threadIdx.x; i < n; i += PLAN_NT)
     if (ok(i)) {
       atomicMin(&to.owner[dst[i]], i);
       if (same) atomicOr(&to.role[src[i]], 1);
     }
-  __threadfence();
-  __syncthreads();
+  sync_agent();
   for (int i = threadIdx.x; i < n; i += PLAN_NT) {
     bool good = ok(i) && ld_agent(&to.owner[dst[i]]) == i;
     if (good && same) good = !ld_agent(&to.role[dst[i]]);
     if (!good && (src[i] >= 0 || dst[i] >= 0)) atomicOr(to.status, TPPSD_STATUS_SEQUENCE);
-    if (good && from.lens[src[i]] > to.max_events) {
-      atomicOr(to.status, TPPSD_STATUS_CAPACITY);
-      good = false;
-    }
     to.p_seq[i] = good ? 1 : 0;
   }
 }
+__device__ __forceinline__ bool pair_goes(const CacheDev &to, const CacheDev &from, int n, const int32_t *src,
+                                          const int32_t *dst, int i, bool same) {
+  return n <= FEW_PAIRS ? pair_stands(to, from, n, src, dst, i, same) : to.p_seq[i] != 0;
+}
 
-// lets go what the destination holds, and (copies) marks the source's pages
-__device__ void dst_clear(const CacheDev &c, int d) {
-  const int held = c.held[d];
-  for (int j = threadIdx.x; j < held; j += blockDim.x) {
-    int32_t *e = &c.table[(size_t)d * c.NP + j];
-    page_drop(c, *e);
-    *e = -1;
+// open rows of a source sequence (len mod 64 of them) into the destination's
+// ring, of layers l0, l0 + step, ..: 16 bytes a thread, the rows of all heads and
+// sides one after the other
+__device__ void copy_tail(const CacheDev &to, const CacheDev &from, int l0, int step, int s, int d, int len) {
+  const int open = len % CACHE_BLOCK, slot0 = len / CACHE_BLOCK * CACHE_BLOCK % CACHE_RING;
+  if (open == 0) return;
+  const int row16 = to.dh * (to.bf16 ? 2 : 4) / 16, side16 = CACHE_RING * row16, sides = to.KV * 2;   // 16-byte words
+  const int sh = __builtin_ctz(row16), word = threadIdx.x & (row16 - 1), rows = blockDim.x >> sh;
+  const int r0 = threadIdx.x >> sh, q = rows / open, rem = rows - q * open;
+  for (int layer = l0; layer < to.L; layer += step) {
+    const uint4 *a = (const uint4 *)from.tails + (((size_t)layer * from.S + s) * sides) * side16 + slot0 * row16 + word;
+    uint4 *b = (uint4 *)to.tails + (((size_t)layer * to.S + d) * sides) * side16 + slot0 * row16 + word;
+    int side = r0 / open, r = r0 - side * open;
+    while (side < sides) {
+      const size_t at = (size_t)side * side16 + r * row16;
+      b[at] = a[at];
+      r += rem;
+      side += q;
+      if (r >= open) r -= open, ++side;
+    }
   }
 }
 
-// open rows of a source sequence (len mod 64 of them) into the destination's ring, 16 bytes a thread
-__device__ void copy_tail(const CacheDev &to, const CacheDev &from, int layer, int s, int d, int len) {
-  const int e = to.bf16 ? 2 : 4, open = len % CACHE_BLOCK, slot0 = len / CACHE_BLOCK * CACHE_BLOCK % CACHE_RING;
-  const int row16 = to.dh * e / 16, side16 = CACHE_RING * row16;   // 16-byte words
-  const uint4 *a = (const uint4 *)from.tails + ((size_t)layer * from.S + s) * to.KV * 2 * side16 + slot0 * row16;
-  uint4 *b = (uint4 *)to.tails + ((size_t)layer * to.S + d) * to.KV * 2 * side16 + slot0 * row16;
-  const int n = open * row16;
-  for (int i = threadIdx.x; i < to.KV * 2 * n; i += blockDim.x) {
-    const int side = i / n, j = i - side * n;
-    b[(size_t)side * side16 + j] = a[(size_t)side * side16 + j];
-  }
-}
-
-// grid (pairs, 1 + layers): table and counters, then each layer's open rows
-__global__ void k_cache_fork(CacheDev c, const int32_t *src, const int32_t *dst) {
+// grid (pairs, 1 + groups of layers): the table and counters, then the layers' open rows
+__global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int32_t *src, const int32_t *dst) {
   const int i = blockIdx.x;
-  if (!c.p_seq[i]) return;
+  if (!pair_goes(c, c, n, src, dst, i, true)) return;
   const int s = src[i], d = dst[i], len = c.lens[s], np = len / CACHE_BLOCK;
   if (blockIdx.y > 0) {
-    copy_tail(c, c, blockIdx.y - 1, s, d, len);
+    copy_tail(c, c, blockIdx.y - 1, gridDim.y - 1, s, d, len);
     return;
   }
-  dst_clear(c, d);
+  pages_drop(c, d, 0, c.held[d]);
   __syncthreads();
   for (int j = threadIdx.x; j < np; j += blockDim.x) {
     const int page = c.table[(size_t)s * c.NP + j];
@@ -353,15 +413,23 @@ __global__ void k_cache_fork(CacheDev c, const int32_t *src, const int32_t *dst)
   }
 }
 
-__global__ void k_copy_mark(CacheDev to, CacheDev from, const int32_t *src, const int32_t *dst) {
-  const int i = blockIdx.x;
-  if (!to.p_seq[i]) return;
-  const int s = src[i], d = dst[i], np = from.lens[s] / CACHE_BLOCK;
-  dst_clear(to, d);
+// the source's pages that move (its bitmap `mark` is zero between calls); verdicts into to.p_seq
+__global__ __launch_bounds__(256) void k_copy_mark(CacheDev to, CacheDev from, int n, const int32_t *src,
+                                                   const int32_t *dst) {
+  const int i = blockIdx.x, s = src[i], d = dst[i];
+  bool go = pair_goes(to, from, n, src, dst, i, false);
+  if (go && from.lens[s] > to.max_events) {
+    if (threadIdx.x == 0) atomicOr(to.status, TPPSD_STATUS_CAPACITY);
+    go = false;
+  }
+  if (threadIdx.x == 0) to.p_seq[i] = go ? 1 : 0;
+  if (!go) return;
+  const int np = from.lens[s] / CACHE_BLOCK;
   for (int j = threadIdx.x; j < np; j += blockDim.x) {
     const int page = from.table[(size_t)s * from.NP + j];
     atomicOr(&from.mark[page >> 5], 1u << (page & 31));
   }
+  pages_drop(to, d, 0, to.held[d]);
   __syncthreads();
   if (threadIdx.x == 0) to.lens[d] = to.held[d] = to.low[d] = to.pend[d] = 0;
 }
@@ -378,6 +446,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev fro
     to.refs[page] = 0;
     atomicAnd(&to.freeb[page >> 5], ~(1u << (page & 31)));
   }
+  for (int w = threadIdx.x; w < (from.n_pages + 31) / 32; w += PLAN_NT) from.mark[w] = 0u;
   if (threadIdx.x == 0) {
     to.counts[1] = fits ? n : -1;
     if (fits && n > 0) to.counts[2] = to.list[n - 1] >> 5;
@@ -385,27 +454,28 @@ __global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev fro
   }
 }
 
-// grid.x = n (1 + L) workgroups for the sequences, the rest for the pages
-__global__ void k_copy_data(CacheDev to, CacheDev from, int n, const int32_t *src, const int32_t *dst) {
+// grid.x = n Y workgroups for the sequences (table and counters, Y - 1 groups of layers), the rest for the pages
+__global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, int n, int Y, const int32_t *src,
+                                                   const int32_t *dst) {
   const int pages = to.counts[1];
   if (pages < 0) return;
-  const int seq_wgs = n * (1 + to.L);
+  const int seq_wgs = n * Y;
   if ((int)blockIdx.x < seq_wgs) {
-    const int i = blockIdx.x % n, layer = (int)blockIdx.x / n - 1;
+    const int i = blockIdx.x % n, y = (int)blockIdx.x / n;
     if (!to.p_seq[i]) return;
     const int s = src[i], d = dst[i], len = from.lens[s], np = len / CACHE_BLOCK;
-    if (layer >= 0) {
-      copy_tail(to, from, layer, s, d, len);
-      return;
-    }
-    for (int j = threadIdx.x; j < np; j += blockDim.x) {
-      const int page = from.map[from.table[(size_t)s * from.NP + j]];
-      to.table[(size_t)d * to.NP + j] = page;
-      atomicAdd(&to.refs[page], 1);
-    }
-    if (threadIdx.x == 0) {
-      to.lens[d] = len;
-      to.held[d] = to.low[d] = np;
+    if (y > 0) {
+      copy_tail(to, from, y - 1, Y - 1, s, d, len);
+    } else {
+      for (int j = threadIdx.x; j < np; j += blockDim.x) {
+        const int page = from.map[from.table[(size_t)s * from.NP + j]];
+        to.table[(size_t)d * to.NP + j] = page;
+        atomicAdd(&to.refs[page], 1);
+      }
+      if (threadIdx.x == 0) {
+        to.lens[d] = len;
+        to.held[d] = to.low[d] = np;
+      }
     }
     return;
   }
@@ -589,7 +659,10 @@ void launch_cache_reset(const CacheDev &c, hipStream_t st) {
 }
 
 void launch_cache_begin(const CacheDev &c, const CacheBegin &b, hipStream_t st) {
-  k_cache_begin<<<1, std::min(PLAN_NT, (b.B + 63) / 64 * 64), 0, st>>>(c, b);
+  const int nt = std::min(PLAN_NT, (b.B + 63) / 64 * 64);
+  if (b.B <= PLAN_NT) k_cache_begin<1><<<1, nt, 0, st>>>(c, b);
+  else if (b.B <= 4 * PLAN_NT) k_cache_begin<4><<<1, nt, 0, st>>>(c, b);
+  else k_cache_begin<0><<<1, nt, 0, st>>>(c, b);
 }
 
 void launch_cache_append(const CacheDev &c, int layer, int B, int P, const CacheRows &r, hipStream_t st) {
@@ -607,17 +680,21 @@ void launch_cache_truncate(const CacheDev &c, int n, const int32_t *seqs, const 
   k_cache_truncate<<<n, 256, 0, st>>>(c, seqs, lens);
 }
 
+// workgroups that share a sequence's layers (a layer each while that makes some ten thousand)
+static int layer_groups(int L, int n) { return std::max(1, std::min(L, 32768 / n)); }
+
 void launch_cache_fork(const CacheDev &c, int n, const int32_t *src, const int32_t *dst, hipStream_t st) {
-  k_cache_pairs<<<1, PLAN_NT, 0, st>>>(c, c, n, src, dst, 1);
-  k_cache_fork<<<dim3(n, 1 + c.L), 256, 0, st>>>(c, src, dst);
+  if (n > FEW_PAIRS) k_cache_pairs<<<1, PLAN_NT, 0, st>>>(c, c, n, src, dst, 1);
+  k_cache_fork<<<dim3(n, 1 + layer_groups(c.L, n)), 256, 0, st>>>(c, n, src, dst);
 }
 
 void launch_cache_copy(const CacheDev &to, const CacheDev &from, int n, const int32_t *src, const int32_t *dst,
                        hipStream_t st) {
-  k_cache_pairs<<<1, PLAN_NT, 0, st>>>(to, from, n, src, dst, 0);
-  k_copy_mark<<<n, 256, 0, st>>>(to, from, src, dst);
+  if (n > FEW_PAIRS) k_cache_pairs<<<1, PLAN_NT, 0, st>>>(to, from, n, src, dst, 0);
+  k_copy_mark<<<n, 256, 0, st>>>(to, from, n, src, dst);
   k_copy_plan<<<1, PLAN_NT, 0, st>>>(to, from);
-  k_copy_data<<<n * (1 + to.L) + 2048, 256, 0, st>>>(to, from, n, src, dst);
+  const int Y = 1 + layer_groups(to.L, n);
+  k_copy_data<<<n * Y + 2048, 256, 0, st>>>(to, from, n, Y, src, dst);
 }
 
 void launch_cache_read(const CacheDev &c, int layer, int n, const int32_t *seqs, const int32_t *first, int count,
