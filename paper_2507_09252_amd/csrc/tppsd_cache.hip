@@ -492,11 +492,6 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
   }
 }
 
-template <typename ACT> __device__ __forceinline__ size_t v_off(const CacheRows &r, int i, int p, int h, int dh, int j) {
-  return r.v_blocked ? i * r.v_sb + h * r.v_sh + (size_t)(p >> 3) * 8 * dh + j * 8 + (p & 7)
-                     : i * r.v_sb + p * r.v_sp + h * r.v_sh + j;
-}
-
 // Appends to one layer. Grid (row, key/value head, block of positions that the
 // rows reach): the block's rows go through LDS; its new rows into the ring
 // where the ring keeps them (the last two blocks), and a block that becomes
@@ -504,7 +499,9 @@ template <typename ACT> __device__ __forceinline__ size_t v_off(const CacheRows 
 // once and writes one byte per element of a whole block: bound by memory.
 template <typename ACT, int DH>
 __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int P, CacheRows r) {
-  __shared__ ACT rows[2][CACHE_BLOCK][DH];
+  constexpr int LDK = DH + 16 / sizeof(ACT), LDV = CACHE_BLOCK + 4, C8 = DH / 8;
+  __shared__ __align__(16) ACT ks[CACHE_BLOCK][LDK];   // keys, row per position
+  __shared__ __align__(16) ACT vs[DH][LDV];            // values, row per column
   __shared__ float top[2][4];
   const int i = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int s = c.p_seq[i], cnt = c.p_count[i], start = c.p_start[i];
@@ -513,130 +510,114 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int
   const int blk = first + blockIdx.z;
   if (blk > last) return;
   const int base = blk * CACHE_BLOCK, n = min(CACHE_BLOCK, end - base);
-  const int old = max(0, min(start - base, CACHE_BLOCK));   // rows of the block from before (first block only)
-  const bool whole = n == CACHE_BLOCK;
-  ACT *ring[2];
-#pragma unroll
-  for (int sd = 0; sd < 2; ++sd)
-    ring[sd] = (ACT *)c.tails + ((((size_t)layer * c.S + s) * c.KV + h) * 2 + sd) * CACHE_RING * DH;
-  const ACT *K = (const ACT *)r.k, *V = (const ACT *)r.v;
-  // element of a row from before the call's rows, or of the call's
-  auto k_new = [&](int pos, int j) { return K[i * r.k_sb + (size_t)(pos - start) * r.k_sp + h * r.k_sh + j]; };
-  auto v_new = [&](int pos, int j) { return V[v_off<ACT>(r, i, pos - start, h, DH, j)]; };
-  const bool keep = blk >= last - 1;
-  const bool need_old = whole || P > CACHE_BLOCK;
-  for (int x = tid; x < CACHE_BLOCK * DH; x += 256) {
-    const int row = x / DH, j = x - row * DH, pos = base + row, slot = pos % CACHE_RING;
-    ACT kv = 0, vv = 0;
-    if (row < old) {
-      if (need_old) kv = ring[0][slot * DH + j], vv = ring[1][slot * DH + j];
-    } else if (row < n) {
-      kv = k_new(pos, j);
-      vv = v_new(pos, j);
-    }
-    rows[0][row][j] = kv;
-    rows[1][row][j] = vv;
-  }
-  __syncthreads();
-  // the first block's slots may be those of a block that the ring keeps: that
-  // block's rows go in here, behind the reads of the old ones
+  const bool whole = n == CACHE_BLOCK, long_call = P > CACHE_BLOCK;
+  ACT *const ring = (ACT *)c.tails + (((size_t)layer * c.S + s) * c.KV + h) * 2 * CACHE_RING * DH;
+  // The first block's slots may be those of a block that the ring keeps: that
+  // block's rows go in with the first block, behind the reads of the old ones.
   const int later = (last - first) % 2 == 0 ? last : last - 1;
   const bool shares = later > first && start % CACHE_BLOCK != 0;
-  if (blk == first && P > CACHE_BLOCK && old > 0) {   // the attention of this call still needs the old rows
-    ACT *st = (ACT *)c.stash + ((size_t)i * c.KV + h) * 2 * CACHE_BLOCK * DH;
-    for (int x = tid; x < old * DH; x += 256) {
-      st[x] = (&rows[0][0][0])[x];
-      st[CACHE_BLOCK * DH + x] = (&rows[1][0][0])[x];
+  const bool keep = blk >= last - 1 && !(shares && blk == later);
+  // 8 elements of new row p from column j on, of the keys and of the values
+  auto fetch = [&](int p, int j, Eight<ACT> &k, Eight<ACT> &v) {
+    k.load((const ACT *)r.k + i * r.k_sb + (size_t)p * r.k_sp + h * r.k_sh + j);
+    const ACT *vp = (const ACT *)r.v + i * r.v_sb + h * r.v_sh;
+    if (r.v_blocked) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.put(e, vp[(size_t)(p >> 3) * 8 * DH + (j + e) * 8 + (p & 7)]);
+    } else {
+      v.load(vp + (size_t)p * r.v_sp + j);
+    }
+  };
+  float top_k = 0.f, top_v = 0.f;
+  constexpr int IT = (CACHE_BLOCK * C8 + 255) / 256;
+  Eight<ACT> k[IT], v[IT];
+#pragma unroll
+  for (int x = 0; x < IT; ++x) {
+    const int at = min(tid + 256 * x, CACHE_BLOCK * C8 - 1), row = min(at / C8, n - 1), j = at % C8 * 8, pos = base + row;
+    if (pos >= start) {
+      fetch(pos - start, j, k[x], v[x]);
+    } else {
+      k[x].load(ring + pos % CACHE_RING * DH + j);
+      v[x].load(ring + (CACHE_RING + pos % CACHE_RING) * DH + j);
     }
   }
-  if (keep && !(shares && blk == later)) {
-    for (int x = tid + old * DH; x < n * DH; x += 256) {
-      const int slot0 = base % CACHE_RING;
-      ring[0][slot0 * DH + x] = (&rows[0][0][0])[x];
-      ring[1][slot0 * DH + x] = (&rows[1][0][0])[x];
+  if (shares && blk == first) __syncthreads();   // (every wave has its old rows)
+#pragma unroll
+  for (int x = 0; x < IT; ++x) {
+    const int at = tid + 256 * x, row = at / C8, j = at % C8 * 8, pos = base + row;
+    if (at >= CACHE_BLOCK * C8 || row >= n) continue;
+    if (pos < start) {
+      if (long_call) {   // the attention of this call still needs the old rows
+        ACT *st = (ACT *)c.stash + (((size_t)i * c.KV + h) * 2 * CACHE_BLOCK + row) * DH + j;
+        k[x].store(st);
+        v[x].store(st + CACHE_BLOCK * DH);
+      }
+    } else if (keep) {
+      k[x].store(ring + pos % CACHE_RING * DH + j);
+      v[x].store(ring + (CACHE_RING + pos % CACHE_RING) * DH + j);
+    }
+    if (whole) {
+      k[x].store(&ks[row][j]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const ACT kv = k[x].at(e), vv = v[x].at(e);
+        vs[j + e][row] = vv;
+        top_up(top_k, ld(&kv, 0));
+        top_up(top_v, ld(&vv, 0));
+      }
     }
   }
-  if (blk == first && shares) {
-    const int b2 = later * CACHE_BLOCK, n2 = min(CACHE_BLOCK, end - b2);
-    for (int x = tid; x < n2 * DH; x += 256) {
-      const int row = x / DH, j = x - row * DH;
-      ring[0][(b2 % CACHE_RING + row) * DH + j] = k_new(b2 + row, j);
-      ring[1][(b2 % CACHE_RING + row) * DH + j] = v_new(b2 + row, j);
+  if (shares && blk == first) {
+    const int n2 = min(CACHE_BLOCK, end - later * CACHE_BLOCK);
+    for (int at = tid; at < n2 * C8; at += 256) {
+      const int j = at % C8 * 8, pos = later * CACHE_BLOCK + at / C8;
+      Eight<ACT> k2, v2;
+      fetch(pos - start, j, k2, v2);
+      k2.store(ring + pos % CACHE_RING * DH + j);
+      v2.store(ring + (CACHE_RING + pos % CACHE_RING) * DH + j);
     }
   }
   if (!whole) return;
-  // block maxima over finite elements
-  float m[2] = {0.f, 0.f};
-  for (int x = tid; x < CACHE_BLOCK * DH; x += 256)
-#pragma unroll
-    for (int sd = 0; sd < 2; ++sd) {
-      const float a = fabsf(ld((const ACT *)&rows[sd][0][0], x));
-      m[sd] = a < INFINITY ? fmaxf(m[sd], a) : m[sd];
-    }
-#pragma unroll
-  for (int sd = 0; sd < 2; ++sd) {
-    m[sd] = lanes_max(m[sd]);
-    if (lane == 0) top[sd][wave] = m[sd];
-  }
+  top_k = lanes_max(top_k);
+  top_v = lanes_max(top_v);
+  if (lane == 0) top[0][wave] = top_k, top[1][wave] = top_v;
   __syncthreads();
-  const size_t page = (size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk];
-  uint8_t *out = c.pages + (page * c.KV + h) * (2 * CACHE_BLOCK * DH);
-#pragma unroll
-  for (int sd = 0; sd < 2; ++sd) {
-    const int e = scale_exp(fmaxf(fmaxf(top[sd][0], top[sd][1]), fmaxf(top[sd][2], top[sd][3])));
-    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    if (tid == 0) c.scales[(page * c.KV + h) * 2 + sd] = __uint_as_float((uint32_t)(127 + e) << 23);
-    for (int x = tid; x < CACHE_BLOCK * DH / 16; x += 256) {   // 16-byte words
-      uint32_t w[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float f[4];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          int key, col;
-          if (sd == 0) key_at<DH>(x >> 6, x & 63, 4 * q + z, key, col);
-          else value_at(x >> 6, x & 63, 4 * q + z, key, col);
-          f[z] = ld((const ACT *)&rows[sd][key][0], col);
-        }
-        w[q] = codes4(f[0], f[1], f[2], f[3], inv);
-      }
-      *(uint4 *)(out + sd * CACHE_BLOCK * DH + 16 * x) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
+  const size_t tile = ((size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk]) * c.KV + h;
+  seal_page<ACT, DH, 4>(ks, vs, top, c.pages + tile * (2 * CACHE_BLOCK * DH), c.scales + tile * 2);
 }
 
 // Rows first[i] .. first[i] + count - 1 of sequences, as the cache holds them:
-// whole blocks from their codes, the open block from the ring; positions past
-// the sequence are left as they were. Grid (row, head, 64 positions).
+// whole blocks from their codes, through LDS, the open block from the ring;
+// positions past the sequence are left as they were. Grid (row, head, block).
 template <typename ACT, int DH>
 __global__ __launch_bounds__(256) void k_cache_read(CacheDev c, int layer, const int32_t *seqs, const int32_t *first,
                                                     int count, ACT *k, ACT *v) {
-  const int i = blockIdx.x, h = blockIdx.y, s = seqs ? seqs[i] : i;
-  if (s < 0 || s >= c.S) {
-    if (threadIdx.x == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
+  constexpr int LD = DH + 16 / sizeof(ACT), C8 = DH / 8;
+  __shared__ __align__(16) ACT rows[2][CACHE_BLOCK][LD];
+  const int i = blockIdx.x, h = blockIdx.y, s = seqs ? seqs[i] : i, tid = threadIdx.x;
+  const int f = first ? first[i] : 0;
+  if (s < 0 || s >= c.S || f < 0) {
+    if (tid == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
     return;
   }
-  const int end = c.lens[s] + c.pend[s], f = first ? first[i] : 0;
-  if (f < 0) {
-    if (threadIdx.x == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
-    return;
+  const int end = c.lens[s] + c.pend[s], blk = f / CACHE_BLOCK + blockIdx.z, base = blk * CACHE_BLOCK;
+  const int lo = max(f, base), hi = min(base + CACHE_BLOCK, f > end ? f : min(end, count > end - f ? end : f + count));
+  if (lo >= hi) return;
+  const bool whole = base + CACHE_BLOCK <= end;
+  if (whole) {
+    const size_t tile = ((size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk]) * c.KV + h;
+    const u32x4_t *page = (const u32x4_t *)(c.pages + tile * (2 * CACHE_BLOCK * DH));
+    const float sk = c.scales[tile * 2], sv = c.scales[tile * 2 + 1];
+    for (int x = tid; x < CACHE_BLOCK * DH / 8; x += 256)
+      open_word<DH>(x, page[x], sk, sv, [&](bool val, int key, int col, float e) { st(&rows[val][key][col], 0, e); });
+    __syncthreads();
   }
   const ACT *ring = (const ACT *)c.tails + (((size_t)layer * c.S + s) * c.KV + h) * 2 * CACHE_RING * DH;
-  for (int x = threadIdx.x; x < 2 * CACHE_BLOCK * DH; x += 256) {
-    const int sd = x / (CACHE_BLOCK * DH), y = x - sd * CACHE_BLOCK * DH, row = blockIdx.z * CACHE_BLOCK + y / DH;
-    const int j = y % DH;
-    if (row >= count || row >= end - f) continue;
-    const int pos = f + row, blk = pos / CACHE_BLOCK;
-    ACT *out = (sd ? v : k) + (((size_t)i * count + row) * c.KV + h) * DH + j;
-    if ((blk + 1) * CACHE_BLOCK <= end) {
-      const size_t tile = ((size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk]) * c.KV + h;
-      const int key = pos % CACHE_BLOCK;
-      const uint32_t code = c.pages[tile * (2 * CACHE_BLOCK * DH) + sd * CACHE_BLOCK * DH +
-                                    (sd ? value_byte(key, j) : key_byte<DH>(key, j))];
-      st(out, 0, __builtin_amdgcn_cvt_f32_fp8(code, 0) * c.scales[tile * 2 + sd]);
-    } else {
-      *out = ring[(sd * CACHE_RING + pos % CACHE_RING) * DH + j];
-    }
+  for (int x = tid; x < 2 * (hi - lo) * C8; x += 256) {
+    const int sd = x >= (hi - lo) * C8, y = sd ? x - (hi - lo) * C8 : x, pos = lo + y / C8, j = y % C8 * 8;
+    Eight<ACT> w;
+    w.load(whole ? &rows[sd][pos - base][j] : ring + (sd * CACHE_RING + pos % CACHE_RING) * DH + j);
+    w.store((sd ? v : k) + (((size_t)i * count + (pos - f)) * c.KV + h) * DH + j);
   }
 }
 
@@ -699,7 +680,7 @@ void launch_cache_copy(const CacheDev &to, const CacheDev &from, int n, const in
 
 void launch_cache_read(const CacheDev &c, int layer, int n, const int32_t *seqs, const int32_t *first, int count,
                        void *k, void *v, hipStream_t st) {
-  const dim3 grid(n, c.KV, (count + CACHE_BLOCK - 1) / CACHE_BLOCK);
+  const dim3 grid(n, c.KV, (count + 2 * CACHE_BLOCK - 2) / CACHE_BLOCK);   // (blocks that count positions may reach)
   by_width(c, [&](auto act, auto w) {
     typedef decltype(act) ACT;
     k_cache_read<ACT, decltype(w)::value><<<grid, 256, 0, st>>>(c, layer, seqs, first, count, (ACT *)k, (ACT *)v);

@@ -71,29 +71,6 @@ __device__ __forceinline__ f32x4_t mma(short4_t a, short4_t b, f32x4_t c) {
   return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a, b, c, 0, 0, 0);
 }
 
-// 8 elements in registers as 16-byte words (two for fp32), and element e of them
-template <typename ACT> struct Eight {
-  static constexpr int W = sizeof(ACT) * 8 / 16;
-  u32x4_t w[W];
-  __device__ __forceinline__ void load(const ACT *p) {
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = ((const u32x4_t *)p)[i];
-  }
-  __device__ __forceinline__ void store(ACT *p) const {
-#pragma unroll
-    for (int i = 0; i < W; ++i) ((u32x4_t *)p)[i] = w[i];
-  }
-  __device__ __forceinline__ ACT at(int e) const {
-    if constexpr (W == 1) return (ACT)(w[0][e >> 1] >> (16 * (e & 1)));
-    else return __uint_as_float(w[e >> 2][e & 3]);
-  }
-  // (e even first: a bf16 word is put together from its two elements)
-  __device__ __forceinline__ void put(int e, ACT v) {
-    if constexpr (W == 1) w[0][e >> 1] = e & 1 ? w[0][e >> 1] | (uint32_t)v << 16 : (uint32_t)v;
-    else w[e >> 2][e & 3] = __float_as_uint(v);
-  }
-};
-
 // the operand of a query or key row at p (8 elements, 4 for d_head 16), part by part into to(part)
 template <typename ACT, int DH, typename TO> __device__ __forceinline__ void load_k(const ACT *p, TO to) {
   if constexpr (sizeof(ACT) == 2) {
@@ -121,7 +98,6 @@ template <typename ACT, int DH, typename TO> __device__ __forceinline__ void loa
 __device__ __forceinline__ uint32_t bf_bad(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
-__device__ __forceinline__ bool not_finite(float x) { return !(fabsf(x) < INFINITY); }
 
 // The operand of 8 values of a column, four at p and four at p + 16, in parts;
 // clean: those that are not finite as 0, or (bad) 1 in their place and 0 elsewhere.
@@ -441,6 +417,7 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
     constexpr int C8 = DH / 8;                 // pieces of 8 elements of a row
     const CacheRows &src = a.kv;
     int bad = 0;
+    float top_k = 0.f, top_v = 0.f;   // largest finite elements of the first block
     for (int x = tid; x < WIN * C8; x += NT) {
       const int row = x / C8, j = (x - row * C8) * 8, pos = base + row;
       const ACT *kp, *vp;
@@ -468,9 +445,10 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
       kk.store(&win.k[row][j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const ACT v = in ? vv.at(e) : (ACT)0;
+        const ACT v = in ? vv.at(e) : (ACT)0, k = kk.at(e);
         win.v[j + e][row] = v;
         bad |= not_finite(ld(&v, 0));
+        if (ONE && n >= CACHE_BLOCK && row < CACHE_BLOCK) top_up(top_k, ld(&k, 0)), top_up(top_v, ld(&v, 0));
       }
       if (ONE && in && pos >= start) {
         ACT *to = (ACT *)ring + (pos % CACHE_RING) * DH + j;
@@ -481,42 +459,12 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
     any_bad = __syncthreads_or(bad);
     if constexpr (ONE) {
       if (n >= CACHE_BLOCK) {   // the first block is whole: its page
-        float m[2] = {0.f, 0.f};
-        for (int x = tid; x < CACHE_BLOCK * DH; x += NT) {
-          const float kf = fabsf(ld(&win.k[x / DH][x % DH], 0)), vf = fabsf(ld(&win.v[x / CACHE_BLOCK][x % CACHE_BLOCK], 0));
-          m[0] = kf < INFINITY ? fmaxf(m[0], kf) : m[0];
-          m[1] = vf < INFINITY ? fmaxf(m[1], vf) : m[1];
-        }
-        m[0] = lanes_max(m[0]);
-        m[1] = lanes_max(m[1]);
-        if (lane == 0) top[0][wave] = m[0], top[1][wave] = m[1];
+        top_k = lanes_max(top_k);
+        top_v = lanes_max(top_v);
+        if (lane == 0) top[0][wave] = top_k, top[1][wave] = top_v;
         __syncthreads();
         const size_t tile = tile_of(table[ba]);
-#pragma unroll
-        for (int side = 0; side < 2; ++side) {
-          float mx = 0.f;
-#pragma unroll
-          for (int w = 0; w < NW; ++w) mx = fmaxf(mx, top[side][w]);
-          const int e = scale_exp(mx);
-          const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-          if (tid == 0) c.scales[tile * 2 + side] = __uint_as_float((uint32_t)(127 + e) << 23);
-          for (int x = tid; x < CACHE_BLOCK * DH / 16; x += NT) {
-            uint32_t w[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              float f[4];
-#pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                int key, col;
-                if (side == 0) key_at<DH>(x >> 6, x & 63, 4 * q + y, key, col);
-                else value_at(x >> 6, x & 63, 4 * q + y, key, col);
-                f[y] = side == 0 ? ld(&win.k[key][col], 0) : ld(&win.v[col][key], 0);
-              }
-              w[q] = codes4(f[0], f[1], f[2], f[3], inv);
-            }
-            ((uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)))[side * (64 * NU) + x] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
-        }
+        seal_page<ACT, DH, NW>(win.k, win.v, top, c.pages + tile * (2 * CACHE_BLOCK * DH), c.scales + tile * 2);
         __syncthreads();   // (the page is read below, by waves of this workgroup)
       }
     }
