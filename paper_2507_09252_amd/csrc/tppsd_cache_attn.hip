@@ -149,41 +149,45 @@ template <typename ACT, int DH, int MT> struct Rows {
   float scale2;       // scale log2 e: exponentials are one exp2 each
   int g;
 
-  // Scores and probabilities of 64 keys: kf(tile, k step, part) gives the key
+  // A block's 64 keys are taken at once, or, where four tiles' scores fill the
+  // registers, in two halves
+  static constexpr int STEPS = MT == 4 || DH == 128 ? 2 : 1, TILES = 4 / STEPS, HALVES = 2 / STEPS;
+
+  // Scores and probabilities of step w: kf(tile, k step, part) gives the key
   // operand of KP parts, seen(t, key) whether this lane's query of tile t sees it.
   template <int KP, bool MASK, typename KF, typename SEEN>
-  __device__ __forceinline__ void scores(KF kf, SEEN seen, bf16x8_t (&p)[MT][NP][2]) {
-    f32x4_t s[MT][4];
+  __device__ __forceinline__ void scores(int w, KF kf, SEEN seen, bf16x8_t (&p)[MT][NP][HALVES]) {
+    f32x4_t s[MT][TILES];
 #pragma unroll
-    for (int t4 = 0; t4 < 4; ++t4) {
+    for (int k4 = 0; k4 < TILES; ++k4) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t) s[t][t4] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      for (int t = 0; t < MT; ++t) s[t][k4] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < NS; ++ks)
 #pragma unroll
         for (int a = 0; a < KP; ++a) {
-          const kfrag k = kf(t4, ks, a);
+          const kfrag k = kf(TILES * w + k4, ks, a);
 #pragma unroll
           for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int b = 0; b < NP; ++b)
-              if (a + b <= 2) s[t][t4] = mma(k, q[t][b][ks], s[t][t4]);
+              if (a + b <= 2) s[t][k4] = mma(k, q[t][b][ks], s[t][k4]);
         }
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int t4 = 0; t4 < 4; ++t4)
+      for (int k4 = 0; k4 < TILES; ++k4)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (MASK && !seen(t, 16 * t4 + 4 * g + i)) s[t][t4][i] = -INFINITY;
-          mx = fmaxf(mx, s[t][t4][i]);
+          if (MASK && !seen(t, 16 * (TILES * w + k4) + 4 * g + i)) s[t][k4][i] = -INFINITY;
+          mx = fmaxf(mx, s[t][k4][i]);
         }
       mx *= scale2;
       // The running maximum moves only when a score passes it by 2^8: until then
       // probabilities stay below 2^8, which fp32 sums and bf16 operands carry
-      // as well, and a tile costs no exchange between lanes and no rescaling.
+      // as well, and a step costs no exchange between lanes and no rescaling.
       if (__ballot(mx > m[t] + 8.f) != 0ull) {
         const float m_new = fmaxf(m[t], xor32_max(xor16_max(mx)));
         const float alpha = __builtin_amdgcn_exp2f(m[t] - (m_new == -INFINITY ? 0.f : m_new));
@@ -195,17 +199,17 @@ template <typename ACT, int DH, int MT> struct Rows {
       }
       const float ref = m[t] == -INFINITY ? 0.f : m[t];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
+      for (int hf = 0; hf < HALVES; ++hf) {
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          x[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * w + (j >> 2)][j & 3], scale2, -ref));
+          x[j] = __builtin_amdgcn_exp2f(fmaf(s[t][2 * hf + (j >> 2)][j & 3], scale2, -ref));
           if (NP > 1) l[t] += x[j];
         }
         bf16x8_t part[NP];
         split8<NP>(x, part);
 #pragma unroll
-        for (int b = 0; b < NP; ++b) p[t][b][w] = part[b];
+        for (int b = 0; b < NP; ++b) p[t][b][hf] = part[b];
       }
     }
     if (NP == 1) {
@@ -213,24 +217,30 @@ template <typename ACT, int DH, int MT> struct Rows {
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) l1[t] = mma(ones, p[t][0][w], l1[t]);
+        for (int hf = 0; hf < HALVES; ++hf) l1[t] = mma(ones, p[t][0][hf], l1[t]);
     }
   }
-  // o += P V: vf(column tile, half of the keys, part)
-  template <int KP, typename VF> __device__ __forceinline__ void values(VF vf, const bf16x8_t (&p)[MT][NP][2]) {
+  // a block: o += P V, vf(column tile, half of the keys, part)
+  template <int KP, bool MASK, typename KF, typename VF, typename SEEN>
+  __device__ __forceinline__ void block(KF kf, VF vf, SEEN seen) {
 #pragma unroll
-    for (int u = 0; u < NU; ++u)
+    for (int w = 0; w < STEPS; ++w) {
+      bf16x8_t p[MT][NP][HALVES];
+      scores<KP, MASK>(w, kf, seen, p);
 #pragma unroll
-      for (int w = 0; w < 2; ++w)
+      for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int a = 0; a < KP; ++a) {
-          const bf16x8_t v = vf(u, w, a);
+        for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
-          for (int t = 0; t < MT; ++t)
+          for (int a = 0; a < KP; ++a) {
+            const bf16x8_t v = vf(u, HALVES * w + hf, a);
 #pragma unroll
-            for (int b = 0; b < NP; ++b)
-              if (a + b <= 2) o[t][u] = mma(v, p[t][b][w], o[t][u]);
-        }
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+              for (int b = 0; b < NP; ++b)
+                if (a + b <= 2) o[t][u] = mma(v, p[t][b][hf], o[t][u]);
+          }
+    }
   }
   // Where values of a tile are not finite the operands hold 0 in their place;
   // bad(u, w) holds 1 there: NaN for the queries that see such a key, nothing for the others.
@@ -305,6 +315,11 @@ inline int groups_of(int G, int rows, int P, bool one) {
   return one ? 1 : (CACHE_BLOCK - 1 + P + CACHE_BLOCK - 1) / CACHE_BLOCK * x.gpb * x.gh;
 }
 
+// Waves per SIMD that the registers are held to: a workgroup's first and last
+// steps are latency, which others hide (a chunk of 16 x 1001 rows with one wave
+// per SIMD 120 us, with two MEASURE); fp32 rows of 128 columns need them all.
+constexpr int min_waves(int dh, int mt, bool bf16) { return !bf16 ? (dh == 128 ? 1 : 2) : dh * mt <= 64 && mt < 4 ? 4 : 2; }
+
 // Attention of a work item (a row of the batch and a range of its pages) for
 // one key/value head and one group of query rows. The NW waves share the
 // queries and take the pages round robin, each with its own running softmax,
@@ -314,7 +329,7 @@ inline int groups_of(int G, int rows, int P, bool one) {
 // call's rows to the cache as well (ring, and pages of blocks that became
 // whole), so that a decoding step is one launch.
 template <typename ACT, int DH, int MT, int NW, bool ONE>
-__global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAttend a) {
+__global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void k_cache_attend(CacheDev c, CacheAttend a) {
   typedef Rows<ACT, DH, MT> R;
   constexpr int NP = R::NP, NS = R::NS, NU = R::NU, NT = 64 * NW;
   constexpr int WIN = ONE ? 2 * CACHE_BLOCK : CACHE_BLOCK;   // rows as they came that a group may see
@@ -483,10 +498,9 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
       const float ks = lane_val(sc.x, x), vs = lane_val(sc.y, x);
       load_side(vw, tile, 1);
       load_side(kn, tile_of(__builtin_amdgcn_readlane(id, min(x + 1, n - 1))), 0);
-      bf16x8_t p[MT][NP][2];
-      s.template scores<1, false>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
-                                  [](int, int) { return true; }, p);
-      s.template values<1>([&](int u, int w, int) { return dec8(word(vw[u], 2 * w), word(vw[u], 2 * w + 1), vs); }, p);
+      s.template block<1, false>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
+                                 [&](int u, int w, int) { return dec8(word(vw[u], 2 * w), word(vw[u], 2 * w + 1), vs); },
+                                 [](int, int) { return true; });
 #pragma unroll
       for (int u = 0; u < NU; ++u) kw[u] = kn[u];
     }
@@ -497,7 +511,6 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
     // step 0: block ba as it came; ONE, past its border: 1: block bb as it came, 2: block ba's page
     const int steps = ONE && bb > ba ? 3 : 1;
     for (int st = (wave + NW - (max(j1 - j0, 0)) % NW) % NW; st < steps; st += NW) {
-      bf16x8_t p[MT][NP][2];
       if (ONE && st == 2) {
         const size_t tile = tile_of(table[ba]);
         uint4 kw[NU], vw[NU];
@@ -505,9 +518,10 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
         load_side(vw, tile, 1);
         const float ks = c.scales[tile * 2], vs = c.scales[tile * 2 + 1];
         auto seen = [&](int t, int) { return s.pos[t] / CACHE_BLOCK > ba; };
-        s.template scores<1, true>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); }, seen, p);
-        s.template values<1>([&](int u, int w, int) {
-          return dec8(drop_codes(word(vw[u], 2 * w)), drop_codes(word(vw[u], 2 * w + 1)), vs); }, p);
+        s.template block<1, true>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
+                                  [&](int u, int w, int) {
+                                    return dec8(drop_codes(word(vw[u], 2 * w)), drop_codes(word(vw[u], 2 * w + 1)), vs);
+                                  }, seen);
         if (any_bad)   // 1.0 (code 0x38) where a code is NaN
           s.poison([&](int u, int w) {
             return dec8((nan_codes(word(vw[u], 2 * w)) >> 7) * 0x38u, (nan_codes(word(vw[u], 2 * w + 1)) >> 7) * 0x38u, 1.f); }, seen);
@@ -516,16 +530,18 @@ __global__ __launch_bounds__(64 * NW) void k_cache_attend(CacheDev c, CacheAtten
       const int b = ba + st, w0 = st * CACHE_BLOCK;
       auto seen = [&](int t, int key) { return s.pos[t] / CACHE_BLOCK == b && b * CACHE_BLOCK + key <= s.pos[t]; };
       kfrag kr[NP][NS];
-      s.template scores<NP, true>([&](int t4, int k2, int part) {
-        if (part == 0)
-          load_k<ACT, DH>(&win.k[w0 + 16 * t4 + rr][DH >= 32 ? 32 * k2 + 8 * g : 4 * g], [&](int x) -> kfrag & { return kr[x][k2]; });
-        return kr[part][k2];
-      }, seen, p);
       bf16x8_t vr[NP];
-      s.template values<NP>([&](int u, int w, int part) {
-        if (part == 0) value8<NP>(&win.v[16 * u + rr][w0 + 32 * w + 4 * g], any_bad != 0, vr);
-        return vr[part];
-      }, p);
+      s.template block<NP, true>(
+          [&](int t4, int k2, int part) {
+            if (part == 0)
+              load_k<ACT, DH>(&win.k[w0 + 16 * t4 + rr][DH >= 32 ? 32 * k2 + 8 * g : 4 * g], [&](int x) -> kfrag & { return kr[x][k2]; });
+            return kr[part][k2];
+          },
+          [&](int u, int w, int part) {
+            if (part == 0) value8<NP>(&win.v[16 * u + rr][w0 + 32 * w + 4 * g], any_bad != 0, vr);
+            return vr[part];
+          },
+          seen);
       if (any_bad)
         s.poison([&](int u, int w) { return bad8(&win.v[16 * u + rr][w0 + 32 * w + 4 * g]); }, seen);
     }
