@@ -426,7 +426,7 @@ class Cache:
         self.ws = torch.zeros(n.value, dtype=torch.uint8, device=device)
         h = c_void_p()
         _check(lib().tppsd_cache_create(ctypes.byref(cfg), _ptr(self.ws), n.value, ctypes.byref(h)))
-        self.handle = h
+        self.handle, self._dev = h, self.ws.get_device()
         np_ = (max_events + CACHE_BLOCK - 1) // CACHE_BLOCK
         self.n_pages = n_pages or np_ * max_seqs
         L, S, KV, dh, N = n_layers, max_seqs, n_kv_heads, d_head, self.n_pages
@@ -446,35 +446,43 @@ class Cache:
             _lib.tppsd_cache_destroy(self.handle)
             self.handle = None
 
+    # (decoding loops call these once per layer and step: plain integers go to
+    # the library, and a tensor's properties are looked at once)
     def _call(self, fn, *args):
         """The entry point on this cache's device and that device's current stream."""
-        dev = self.ws.device.index
+        dev = self._dev
         if dev == torch.cuda.current_device():
-            _check(fn(*args, _stream()))
+            _check(fn(self.handle, *args, torch.cuda.current_stream(dev).cuda_stream))
         else:
             with torch.cuda.device(dev):
-                _check(fn(*args, _stream()))
+                _check(fn(self.handle, *args, torch.cuda.current_stream(dev).cuda_stream))
 
     def _ints(self, t, n=None, what="index"):
+        """Address of an index vector (None: NULL)."""
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.device != self.ws.device or t.dim() != 1 or not t.is_contiguous():
+        if t.dtype is not torch.int32 or t.get_device() != self._dev or t.dim() != 1 or not t.is_contiguous():
             raise TppsdError(1, f"{what} must be a contiguous int32 vector on {self.ws.device}")
         if n is not None and t.numel() != n:
             raise TppsdError(1, f"{what} has {t.numel()} elements, needs {n}")
-        return t
+        return t.data_ptr()
 
     def _row(self, t, heads, what):
+        """Address and row stride of rows [B, n_new, heads, d_head]."""
         B, P = self._plan
-        if t.dtype != self.dtype or t.device != self.ws.device or tuple(t.shape) != (B, P, heads, self.d_head):
-            raise TppsdError(1, f"{what} must be {self.dtype} [{B}, {P}, {heads}, {self.d_head}] on {self.ws.device}")
-        ld = t.stride(1) if P > 1 else (t.stride(0) if B > 1 else heads * self.d_head)
-        if t.stride(3) != 1 or (heads > 1 and t.stride(2) != self.d_head) or (B > 1 and t.stride(0) != P * ld):
+        dh = self.d_head
+        if t.dtype is not self.dtype or t.get_device() != self._dev or t.shape != (B, P, heads, dh):
+            raise TppsdError(1, f"{what} must be {self.dtype} [{B}, {P}, {heads}, {dh}] on {self.ws.device}")
+        if t.is_contiguous():
+            return t.data_ptr(), heads * dh
+        sb, sp, sh, sd = t.stride()
+        ld = sp if P > 1 else (sb if B > 1 else heads * dh)
+        if sd != 1 or (heads > 1 and sh != dh) or (B > 1 and sb != P * ld):
             raise TppsdError(1, f"{what}: heads must be contiguous and rows evenly spaced")
         return t.data_ptr(), ld
 
     def tppsd_cache_reset(self):
-        self._call(lib().tppsd_cache_reset, self.handle)
+        self._call(_lib.tppsd_cache_reset)
         self._plan = None
 
     def tppsd_cache_begin(self, n_new: int, seqs: Optional[torch.Tensor] = None,
@@ -482,8 +490,8 @@ class Cache:
         """batch: rows of the call (default: as many as seqs or counts has, or every sequence)."""
         if batch is None:
             batch = seqs.numel() if seqs is not None else counts.numel() if counts is not None else self.max_seqs
-        seqs, counts = self._ints(seqs, batch, "seqs"), self._ints(counts, batch, "counts")
-        self._call(lib().tppsd_cache_begin, self.handle, batch, n_new, _ptr(seqs), _ptr(counts))
+        self._call(_lib.tppsd_cache_begin, batch, n_new, self._ints(seqs, batch, "seqs"),
+                   self._ints(counts, batch, "counts"))
         self._plan = (batch, n_new)
 
     def _planned(self):
@@ -494,7 +502,7 @@ class Cache:
         self._planned()
         (kp, ldk), (vp, ldv) = self._row(k, self.n_kv_heads, "k"), self._row(v, self.n_kv_heads, "v")
         r = CacheRowsC(None, kp, vp, None, 0, ldk, ldv, 0)
-        self._call(lib().tppsd_cache_append, self.handle, layer, ctypes.byref(r))
+        self._call(_lib.tppsd_cache_append, layer, ctypes.byref(r))
 
     def tppsd_cache_attend(self, layer: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                            out: Optional[torch.Tensor] = None, scale: Optional[float] = None,
@@ -506,35 +514,31 @@ class Cache:
         (qp, ldq), (op, ldo) = self._row(q, self.n_heads, "q"), self._row(out, self.n_heads, "out")
         (kp, ldk), (vp, ldv) = self._row(k, self.n_kv_heads, "k"), self._row(v, self.n_kv_heads, "v")
         r = CacheRowsC(qp, kp, vp, op, ldq, ldk, ldv, ldo)
-        self._call(lib().tppsd_cache_attend, self.handle, layer, ctypes.byref(r),
-                                        self.d_head ** -0.5 if scale is None else scale, int(sink))
+        self._call(_lib.tppsd_cache_attend, layer, ctypes.byref(r),
+                   self.d_head ** -0.5 if scale is None else scale, int(sink))
         return out
 
     def tppsd_cache_commit(self, accept: Optional[torch.Tensor] = None):
         self._planned()
-        accept = self._ints(accept, self._plan[0], "accept")
-        self._call(lib().tppsd_cache_commit, self.handle, _ptr(accept))
+        self._call(_lib.tppsd_cache_commit, self._ints(accept, self._plan[0], "accept"))
         self._plan = None
 
     def tppsd_cache_truncate(self, seqs: torch.Tensor, lens: Optional[torch.Tensor] = None):
-        seqs = self._ints(seqs, None, "seqs")
-        lens = self._ints(lens, seqs.numel(), "lens")
-        self._call(lib().tppsd_cache_truncate, self.handle, seqs.numel(), _ptr(seqs), _ptr(lens))
+        n = seqs.numel()
+        self._call(_lib.tppsd_cache_truncate, n, self._ints(seqs, n, "seqs"), self._ints(lens, n, "lens"))
         self._plan = None
 
     def tppsd_cache_fork(self, src: torch.Tensor, dst: torch.Tensor):
-        src = self._ints(src, None, "src")
-        dst = self._ints(dst, src.numel(), "dst")
-        self._call(lib().tppsd_cache_fork, self.handle, src.numel(), _ptr(src), _ptr(dst))
+        n = src.numel()
+        self._call(_lib.tppsd_cache_fork, n, self._ints(src, n, "src"), self._ints(dst, n, "dst"))
         self._plan = None
 
     def tppsd_cache_copy(self, source: "Cache", src: torch.Tensor, dst: torch.Tensor):
         """Sequences src of the cache `source` into this cache's sequences dst."""
-        src = self._ints(src, None, "src")
-        dst = self._ints(dst, src.numel(), "dst")
+        n = src.numel()
         if source.ws.device != self.ws.device:
             raise TppsdError(1, "caches lie on different devices")
-        self._call(lib().tppsd_cache_copy, self.handle, source.handle, src.numel(), _ptr(src), _ptr(dst))
+        self._call(_lib.tppsd_cache_copy, source.handle, n, self._ints(src, n, "src"), self._ints(dst, n, "dst"))
         self._plan = None
 
     def tppsd_cache_read(self, layer: int, first: Optional[torch.Tensor], count: int,
@@ -542,16 +546,16 @@ class Cache:
                          seqs: Optional[torch.Tensor] = None):
         """(k, v) [n, count, n_kv_heads, d_head] of positions first .. first + count - 1 (default 0)."""
         n = seqs.numel() if seqs is not None else first.numel() if first is not None else self.max_seqs
-        first, seqs = self._ints(first, n, "first"), self._ints(seqs, n, "seqs")
         shape = (n, count, self.n_kv_heads, self.d_head)
         if k is None:
             k = torch.zeros(shape, dtype=self.dtype, device=self.ws.device)
         if v is None:
             v = torch.zeros(shape, dtype=self.dtype, device=self.ws.device)
         for t in (k, v):
-            if tuple(t.shape) != shape or t.dtype != self.dtype or t.device != self.ws.device or not t.is_contiguous():
+            if t.shape != shape or t.dtype is not self.dtype or t.get_device() != self._dev or not t.is_contiguous():
                 raise TppsdError(1, f"outputs must be contiguous {self.dtype} {list(shape)}")
-        self._call(lib().tppsd_cache_read, self.handle, layer, n, _ptr(seqs), _ptr(first), count, _ptr(k), _ptr(v))
+        self._call(_lib.tppsd_cache_read, layer, n, self._ints(seqs, n, "seqs"), self._ints(first, n, "first"), count,
+                   k.data_ptr(), v.data_ptr())
         return k, v
 
     def tppsd_cache_status(self) -> int:
