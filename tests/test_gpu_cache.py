@@ -475,3 +475,58 @@ def test_results_repeat():
         b.c.tppsd_cache_begin(5)
         outs.append(b.c.tppsd_cache_attend(0, *(b.rand(2, 5, 2, 64) for _ in range(3))))
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+@pytest.mark.parametrize("prec,H,KV,dh,P,n", [("bf16", 80, 1, 16, 3, 130), ("fp32", 70, 1, 32, 1, 70),
+                                              ("bf16", 33, 1, 128, 2, 200), ("bf16", 5, 5, 64, 66, 1)])
+def test_more_heads_than_query_rows(prec, H, KV, dh, P, n):
+    """Query heads of one key/value head that take several groups of rows a position."""
+    b = Both(1, H, KV, dh, prec, 2, n + 2 * P, seed=H)
+    b.begin(n, counts=[n, n // 2])
+    b.step(queries=False)
+    b.commit()
+    for counts in (None, [P, 0]):
+        b.begin(P, counts=counts, batch=2)
+        b.step()
+        b.commit()
+    b.same(0)
+
+
+@pytest.mark.parametrize("S", [1025, 4097, 5000])
+def test_many_rows(S):
+    """Batches of several rows a thread of the plan, ragged, with fewer pages than they ask for at last."""
+    rng = np.random.default_rng(S)
+    b = Both(1, 1, 1, 16, "bf16", S, 256, n_pages=S, seed=S)
+    for P, some in ((70, False), (64, True), (100, True)):
+        seqs = rng.permutation(S)[:S - 5].tolist() if some else None
+        B = len(seqs) if some else S
+        b.begin(P, seqs=seqs, counts=rng.integers(0, P + 1, B).tolist())
+        b.step(queries=False)
+        b.commit()
+    b.same()
+    assert b.r.status == PAGES
+
+
+@pytest.mark.parametrize("n", [255, 256, 257, 700])
+def test_long_lists_of_pairs(n):
+    """Forks and copies of few and of many pairs, with bad ones among them: the same rules."""
+    S = 701
+    rng = np.random.default_rng(n)
+    b = Both(2, 1, 1, 16, "bf16", S, 200, seed=n)
+    b.begin(150, counts=rng.integers(0, 151, S).tolist())
+    b.step(queries=False)
+    b.commit()
+    src, dst = rng.integers(0, 40, n).tolist(), (40 + rng.permutation(S - 40)).tolist()[:n]
+    dst += [-1] * (n - len(dst))
+    src[5], dst[7], dst[n - 1], src[n - 2], dst[n - 3] = S, dst[8], 3, -1, -1
+    b.c.tppsd_cache_fork(ints(src), ints(dst))
+    b.r.fork(src, dst)
+    b.same(SEQUENCE)
+    o = Both(2, 1, 1, 16, "bf16", S, 200, seed=1)
+    o.c.tppsd_cache_copy(b.c, ints(src), ints(dst))
+    o.r.copy(b.r, src, dst)
+    o.same(SEQUENCE)
+    o.begin(3)
+    o.step(queries=False)
+    o.commit()
+    o.same()
