@@ -423,6 +423,17 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
       return dec4(word(w[0], t4), sc);
     }
   };
+  // page ids and scales of the wave's next 64 pages, one per lane, and its first
+  // page's keys: on their way while the rows below are
+  int jc = j0 + wave, id = 0;
+  float2 sc = {0.f, 0.f};
+  uint4 kw[NU];
+  auto fetch = [&] {
+    id = table[min(jc + lane * NW, j1 - 1)];
+    sc = *(const float2 *)(c.scales + tile_of(id) * 2);
+    load_side(kw, tile_of(__builtin_amdgcn_readlane(id, 0)), 0);
+  };
+  if (jc < j1) fetch();
   int any_bad = 0;
   if (mine) {
     const int base = ba * CACHE_BLOCK, n = min(end - base, WIN);
@@ -486,13 +497,9 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   }
 
   // ---- the pages that every query sees ------------------------------------
-  for (int jc = j0 + wave; jc < j1; jc += 64 * NW) {
-    // page ids and scales of the wave's next 64 pages, one per lane
-    const int jl = min(jc + lane * NW, j1 - 1), n = min(64, (j1 - jc + NW - 1) / NW);
-    const int id = table[jl];
-    const float2 sc = *(const float2 *)(c.scales + tile_of(id) * 2);
-    uint4 kw[NU], vw[NU], kn[NU];
-    load_side(kw, tile_of(__builtin_amdgcn_readlane(id, 0)), 0);
+  while (jc < j1) {
+    const int n = min(64, (j1 - jc + NW - 1) / NW);
+    uint4 vw[NU], kn[NU];
     for (int x = 0; x < n; ++x) {
       const size_t tile = tile_of(__builtin_amdgcn_readlane(id, x));
       const float ks = lane_val(sc.x, x), vs = lane_val(sc.y, x);
@@ -504,6 +511,8 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
 #pragma unroll
       for (int u = 0; u < NU; ++u) kw[u] = kn[u];
     }
+    jc += 64 * NW;
+    if (jc < j1) fetch();
   }
 
   // ---- the queries' own blocks, as their rows came -------------------------
