@@ -92,6 +92,7 @@ struct CacheAttend {
   float scale;
   int sink;
   int zero;           // rows that are left out are written as zeros
+  int whole;          // (set by the launcher) rows are not split: no work items
 };
 
 void launch_cache_reset(const CacheDev &c, hipStream_t st);

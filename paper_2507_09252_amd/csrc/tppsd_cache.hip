@@ -233,17 +233,16 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
     mine.b += top_of(r);
     mine.top = max(mine.top, top_of(r));
   });
-  if (avail < all.a) all = block_sums(mine, &before, sums);   // (rows were left out)
+  if (avail < all.a && b.split_target > 0) all = block_sums(mine, &before, sums);   // (rows were left out)
   // Work items. Rows of about equal length that fill the chip are taken whole.
   // Otherwise pages are dealt out in pieces of a workgroup's share, or, where
   // many rows leave many remainders, of a third of it. Pieces of a row have
   // adjoining slots for their partial states.
+  if (b.split_target <= 0) return;   // (the attention reads the rows)
   int chunk = INT32_MAX;
-  if (b.split_target > 0) {
-    const int share = (all.b + b.split_target - 1) / b.split_target, parts = b.B * 4 <= b.split_target ? 1 : 3;
-    if (all.top > share + share / 4)
-      chunk = max(CACHE_MIN_PIECE, (all.b + parts * b.split_target - 1) / (parts * b.split_target));
-  }
+  const int share = (all.b + b.split_target - 1) / b.split_target, parts = b.B * 4 <= b.split_target ? 1 : 3;
+  if (all.top > share + share / 4)
+    chunk = max(CACHE_MIN_PIECE, (all.b + parts * b.split_target - 1) / (parts * b.split_target));
   auto pieces = [&](int top) { return top <= chunk ? 1 : (top + chunk - 1) / chunk; };
   mine = {0, 0, 0};
   each(false, [&](int, Row &r) {

@@ -356,8 +356,17 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, rr = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, G = c.H / c.KV, item = blockIdx.x;
-  if (item >= c.counts[0]) return;
-  const CacheItem it = c.items[item];
+  CacheItem it;
+  if (a.whole) {   // rows are not split: the plan's rows say it all
+    it.row = item;
+    it.seq = c.p_seq[item], it.start = c.p_start[item], it.count = c.p_count[item];
+    it.lo = it.piece = it.slot0 = 0;
+    it.hi = it.count > 0 ? (it.start + it.count - 1) / CACHE_BLOCK : 0;
+    it.pieces = 1;
+  } else {
+    if (item >= c.counts[0]) return;
+    it = c.items[item];
+  }
   const int i = it.row, cnt = it.count, start = it.start, seq = it.seq;
   const size_t head0 = (size_t)h * G * DH;
   ACT *const O = (ACT *)a.o;
@@ -516,9 +525,9 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   }
 
   // ---- the queries' own blocks, as their rows came -------------------------
+  // step 0: block ba as it came; ONE, past its border: 1: block bb as it came, 2: block ba's page
+  const int steps = ONE && bb > ba ? 3 : 1;
   if (mine) {
-    // step 0: block ba as it came; ONE, past its border: 1: block bb as it came, 2: block ba's page
-    const int steps = ONE && bb > ba ? 3 : 1;
     for (int st = (wave + NW - (max(j1 - j0, 0)) % NW) % NW; st < steps; st += NW) {
       if (ONE && st == 2) {
         const size_t tile = tile_of(table[ba]);
@@ -560,10 +569,11 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   // ---- sums over the lane groups, then over the waves ----------------------
 #pragma unroll
   for (int t = 0; t < MT; ++t) s.l[t] = NP == 1 ? s.l1[t][0] : xor32_sum(xor16_sum(s.l[t]));
-  // wave 0 gets the state of all waves
-  auto fold_waves = [&] {
+  // wave 0 gets the state of the first `busy` waves (the others have none)
+  auto fold_waves = [&](int busy) {
 #pragma unroll
     for (int half = NW / 2; half > 0; half >>= 1) {
+      if (busy <= half) continue;
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
@@ -580,7 +590,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
       if (half > 1) __syncthreads();
     }
   };
-  fold_waves();
+  fold_waves(max(j1 - j0, 0) + (mine ? steps : 0));
   if (it.pieces > 1) {
     // [slot][head][group][o, m, l][64]: lane by lane. The state goes out and comes
     // in by accesses that are coherent over the whole GPU (its dies have an L2
@@ -630,7 +640,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
                return (f32x4_t){get(at), get(at + 1), get(at + 2), get(at + 3)};
              });
     }
-    fold_waves();
+    fold_waves(it.pieces);
   }
   if (wave != 0) return;
   // ---- normalise and store: lane (rr, g) holds columns 16 u + 4 g .. + 3 of query rr ----
@@ -704,11 +714,13 @@ size_t cache_part_floats(const CacheDev &c) {
   return std::min<size_t>(6 * CACHE_SPLIT_WAVES / 4, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
 }
 
-void launch_cache_attend(const CacheDev &c, const CacheAttend &a, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+void launch_cache_attend(const CacheDev &c, const CacheAttend &call, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {
+  CacheAttend a = call;
   const long R = (long)a.P * (c.H / c.KV);
   const bool one = one_group(c, a.P);
   const int waves = waves_of(c, a.B, a.P);
   const int target = cache_split_target(c, a.B, a.P), items = a.B + (target ? 3 * target + 1 : 0);
+  a.whole = target == 0;
   if (!one) launch_cache_append(c, a.layer, a.B, a.P, a.kv, st);
   auto go = [&](auto act, auto width) {
     typedef decltype(act) ACT;
