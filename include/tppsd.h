@@ -475,8 +475,9 @@ int tppsd_cache_append(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
  * value 0 (the 1 + sum f of AttNHP). Scores, the softmax's maximum and sum and
  * the output are accumulated in fp32. A position whose own visible keys or
  * values are not finite gets NaN; positions that do not see them are not
- * touched. o may be q's memory, not k's or v's. Errors: as tppsd_cache_append, scale not
- * positive and finite: TPPSD_E_ARG. */
+ * touched. o may be q's memory, not k's or v's. Errors: as tppsd_cache_append; TPPSD_E_ARG
+ * also for a scale that is not positive and finite, and for more than 65535
+ * groups of query rows (beyond 2^18 positions of eight query heads a key/value head of 128). */
 int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, float scale, int sink,
                        hipStream_t stream);
 

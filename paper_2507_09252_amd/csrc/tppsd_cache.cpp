@@ -192,7 +192,7 @@ int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, c
   if (B < 1 || B > c->d.S) return fail(TPPSD_E_ARG, "batch %d outside 1..%d", B, c->d.S);
   if (n_new < 1 || n_new > c->d.max_events)
     return fail(TPPSD_E_ARG, "n_new %d outside 1..%d", n_new, c->d.max_events);
-  if ((long long)n_new * (c->d.H / c->d.KV) > (1LL << 30) || n_new / CACHE_BLOCK > 65000)
+  if (n_new / CACHE_BLOCK > 65000)
     return fail(TPPSD_E_ARG, "n_new %d too large", n_new);
   CacheBegin b{};
   b.B = B;
@@ -224,6 +224,8 @@ int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
   if (int rc = check_rows(c->d, rows->q, rows->ldq, c->d.H, "q")) return rc;
   if (int rc = check_rows(c->d, rows->o, rows->ldo, c->d.H, "o")) return rc;
   if (!(scale > 0.f) || !std::isfinite(scale)) return fail(TPPSD_E_ARG, "scale must be positive and finite");
+  if (cache_groups(c->d, c->P) > 65535)   // (a dimension of the grid)
+    return fail(TPPSD_E_ARG, "%d positions of %d heads a key/value head are too many for one call", c->P, c->d.H / c->d.KV);
   CacheAttend a{};
   a.q = rows->q;
   a.o = rows->o;

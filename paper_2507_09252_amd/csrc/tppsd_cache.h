@@ -110,6 +110,8 @@ void launch_cache_read(const CacheDev &c, int layer, int n, const int32_t *seqs,
 // items that make a full chip for a batch of B rows of P positions, 0 where
 // rows are not split
 int cache_split_target(const CacheDev &c, int B, int P);
+// groups of query rows of a call of P positions (one grid dimension)
+int cache_groups(const CacheDev &c, int P);
 int cache_max_items(int S, int KV);
 size_t cache_part_floats(const CacheDev &c);
 void launch_cache_attend(const CacheDev &c, const CacheAttend &a, hipStream_t st, hipEvent_t ev0 = nullptr,

@@ -312,12 +312,14 @@ __host__ __device__ inline Group group_of(int G, int rows) {
 }
 inline int groups_of(int G, int rows, int P, bool one) {
   const Group x = group_of(G, rows);
-  return one ? 1 : (CACHE_BLOCK - 1 + P + CACHE_BLOCK - 1) / CACHE_BLOCK * x.gpb * x.gh;
+  // (an int: at most 2^24 + 1 blocks of 64 groups, saturated)
+  const long n = ((long)P + 2 * CACHE_BLOCK - 2) / CACHE_BLOCK * x.gpb * x.gh;
+  return one ? 1 : (int)std::min<long>(n, INT32_MAX);
 }
 
 // Waves per SIMD that the registers are held to: a workgroup's first and last
 // steps are latency, which others hide (a chunk of 16 x 1001 rows with one wave
-// per SIMD 120 us, with two MEASURE); fp32 rows of 128 columns need them all.
+// per SIMD 120 us, with two 71); fp32 rows of 128 columns need them all.
 constexpr int min_waves(int dh, int mt, bool bf16) { return !bf16 ? (dh == 128 ? 1 : 2) : dh * mt <= 64 && mt < 4 ? 4 : 2; }
 
 // Attention of a work item (a row of the batch and a range of its pages) for
@@ -701,7 +703,9 @@ int cache_split_target(const CacheDev &c, int B, int P) {
   return per > full || B * per > CACHE_JOINS ? 0 : (int)(full / per);
 }
 
-// a row, and for a split batch about three times the target more
+int cache_groups(const CacheDev &c, int P) { return call_groups(c, P); }
+
+// items of a batch: one per row, and for a split one about three times the target more
 int cache_max_items(int S, int KV) { return S + 3 * (CACHE_SPLIT_WAVES / 4 / KV + 1) + 2; }
 
 // Partial states: a row of t pages in pieces of C >= pages / (3 target) takes

@@ -99,6 +99,14 @@ def test_calls_refused(lib):
     for B, n in ((0, 1), (4, 1), (1, 0), (1, 201), (-1, 5)):
         assert lib.tppsd_cache_begin(h, B, n, None, None, None) == ARG, (B, n)
     assert lib.tppsd_cache_begin(h, 2, 5, None, None, None) == 5
+    # groups of query rows are a grid dimension: 8 positions of 8 heads a group of 64 rows
+    many = make(lib, n_heads=16, max_events=1 << 20)
+    assert lib.tppsd_cache_reset(many, None) == 5
+    wide_rows = tp.CacheRowsC(p, p, p, p, 512, 64, 64, 512)
+    for n, code in ((1 << 19, ARG), (1 << 18, 5)):
+        assert lib.tppsd_cache_begin(many, 1, n, None, None, None) == 5
+        assert lib.tppsd_cache_attend(many, 0, ctypes.byref(wide_rows), 1.0, 0, None) == code
+    lib.tppsd_cache_destroy(many)
     for layer in (-1, 2):
         assert lib.tppsd_cache_append(h, layer, r, None) == ARG
         assert lib.tppsd_cache_attend(h, layer, r, 1.0, 0, None) == ARG

@@ -507,10 +507,9 @@ def test_many_rows(S):
     assert b.r.status == PAGES
 
 
-@pytest.mark.parametrize("n", [255, 256, 257, 700])
-def test_long_lists_of_pairs(n):
-    """Forks and copies of few and of many pairs, with bad ones among them: the same rules."""
-    S = 701
+@pytest.mark.parametrize("n,S", [(255, 701), (256, 701), (257, 701), (700, 701), (300, 13000)])
+def test_long_lists_of_pairs(n, S):
+    """Forks and copies of few and of many pairs, with bad ones among them, of few and many sequences: the same rules."""
     rng = np.random.default_rng(n)
     b = Both(2, 1, 1, 16, "bf16", S, 200, seed=n)
     b.begin(150, counts=rng.integers(0, 151, S).tolist())
