@@ -92,7 +92,9 @@ struct CacheAttend {
   float scale;
   int sink;
   int zero;           // rows that are left out are written as zeros
-  int whole;          // (set by the launcher) rows are not split: no work items
+  // set by the launcher:
+  int whole;          // rows are not split: no work items
+  int nt_pages;       // pages of a row from which they are read with the non-temporal hint
 };
 
 void launch_cache_reset(const CacheDev &c, hipStream_t st);

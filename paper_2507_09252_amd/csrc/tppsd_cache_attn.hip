@@ -326,11 +326,13 @@ constexpr int min_waves(int dh, int mt, bool bf16) { return !bf16 ? (dh == 128 ?
 // one key/value head and one group of query rows. The NW waves share the
 // queries and take the pages round robin, each with its own running softmax,
 // folded at the end; the splits of a row are joined by the workgroup that
-// finishes last. The item with the row's last pages also takes the blocks that
+// finishes last. HINT: rows of at least nt_pages read them with the non-temporal
+// hint (an instance of its own: a second page loop costs short rows a few
+// per cent in instruction fetches). The item with the row's last pages also takes the blocks that
 // the queries see as their rows came, from LDS. ONE: that item appends the
 // call's rows to the cache as well (ring, and pages of blocks that became
 // whole), so that a decoding step is one launch.
-template <typename ACT, int DH, int MT, int NW, bool ONE>
+template <typename ACT, int DH, int MT, int NW, bool ONE, bool HINT>
 __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void k_cache_attend(CacheDev c, CacheAttend a) {
   typedef Rows<ACT, DH, MT> R;
   constexpr int NP = R::NP, NS = R::NS, NU = R::NU, NT = 64 * NW;
@@ -420,10 +422,14 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   const int32_t *table = c.table + (size_t)seq * c.NP;
   const int j0 = it.lo, j1 = min(it.hi, ba);
   auto tile_of = [&](int page) { return (layer0 + page) * c.KV + h; };
-  auto load_side = [&](uint4 (&w)[NU], size_t tile, int side) {
-    const uint4 *p = (const uint4 *)(c.pages + tile * (2 * CACHE_BLOCK * DH)) + side * (64 * NU) + lane;
+  // (nt: pages that the next pass will not find in a cache pass the caches by)
+  auto load_side = [&](uint4 (&w)[NU], size_t tile, int side, auto nt) {
+    const u32x4_t *p = (const u32x4_t *)(c.pages + tile * (2 * CACHE_BLOCK * DH)) + side * (64 * NU) + lane;
 #pragma unroll
-    for (int u = 0; u < NU; ++u) w[u] = p[64 * u];
+    for (int u = 0; u < NU; ++u) {
+      if constexpr (decltype(nt)::value) w[u] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(p + 64 * u));
+      else w[u] = __builtin_bit_cast(uint4, p[64 * u]);
+    }
   };
   auto word = [](const uint4 &x, int n) { return n == 0 ? x.x : n == 1 ? x.y : n == 2 ? x.z : x.w; };
   auto k_codes = [&](const uint4 (&w)[NU], float sc, int t4, int ks) -> kfrag {
@@ -442,7 +448,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   auto fetch = [&] {
     id = table[min(jc + lane * NW, j1 - 1)];
     sc = *(const float2 *)(c.scales + tile_of(id) * 2);
-    load_side(kw, tile_of(__builtin_amdgcn_readlane(id, 0)), 0);
+    load_side(kw, tile_of(__builtin_amdgcn_readlane(id, 0)), 0, std::false_type{});
   };
   if (jc < j1) fetch();
   int any_bad = 0;
@@ -508,22 +514,30 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
   }
 
   // ---- the pages that every query sees ------------------------------------
-  while (jc < j1) {
-    const int n = min(64, (j1 - jc + NW - 1) / NW);
-    uint4 vw[NU], kn[NU];
-    for (int x = 0; x < n; ++x) {
-      const size_t tile = tile_of(__builtin_amdgcn_readlane(id, x));
-      const float ks = lane_val(sc.x, x), vs = lane_val(sc.y, x);
-      load_side(vw, tile, 1);
-      load_side(kn, tile_of(__builtin_amdgcn_readlane(id, min(x + 1, n - 1))), 0);
-      s.template block<1, false>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
-                                 [&](int u, int w, int) { return dec8(word(vw[u], 2 * w), word(vw[u], 2 * w + 1), vs); },
-                                 [](int, int) { return true; });
+  auto pages = [&](auto nt) {
+    while (jc < j1) {
+      const int n = min(64, (j1 - jc + NW - 1) / NW);
+      uint4 vw[NU], kn[NU];
+      for (int x = 0; x < n; ++x) {
+        const size_t tile = tile_of(__builtin_amdgcn_readlane(id, x));
+        const float ks = lane_val(sc.x, x), vs = lane_val(sc.y, x);
+        load_side(vw, tile, 1, nt);
+        load_side(kn, tile_of(__builtin_amdgcn_readlane(id, min(x + 1, n - 1))), 0, nt);
+        s.template block<1, false>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
+                                   [&](int u, int w, int) { return dec8(word(vw[u], 2 * w), word(vw[u], 2 * w + 1), vs); },
+                                   [](int, int) { return true; });
 #pragma unroll
-      for (int u = 0; u < NU; ++u) kw[u] = kn[u];
+        for (int u = 0; u < NU; ++u) kw[u] = kn[u];
+      }
+      jc += 64 * NW;
+      if (jc < j1) fetch();
     }
-    jc += 64 * NW;
-    if (jc < j1) fetch();
+  };
+  if constexpr (HINT) {
+    if ((end - 1) / CACHE_BLOCK >= a.nt_pages) pages(std::true_type{});   // (uniform)
+    else pages(std::false_type{});
+  } else {
+    pages(std::false_type{});
   }
 
   // ---- the queries' own blocks, as their rows came -------------------------
@@ -534,8 +548,8 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
       if (ONE && st == 2) {
         const size_t tile = tile_of(table[ba]);
         uint4 kw[NU], vw[NU];
-        load_side(kw, tile, 0);
-        load_side(vw, tile, 1);
+        load_side(kw, tile, 0, std::false_type{});
+        load_side(vw, tile, 1, std::false_type{});
         const float ks = c.scales[tile * 2], vs = c.scales[tile * 2 + 1];
         auto seen = [&](int t, int) { return s.pos[t] / CACHE_BLOCK > ba; };
         s.template block<1, true>([&](int t4, int k2, int) { return k_codes(kw, ks, t4, k2); },
@@ -698,6 +712,15 @@ int waves_of(const CacheDev &c, int B, int P) {
 
 }  // namespace
 
+// Pages of a sequence from which they are read with the non-temporal hint: where
+// those of all layers and rows are 384 MiB, which the 256 MB last-level cache
+// does not keep for the next pass. Four layers of 32 x 4600 positions (620 MB)
+// 150 -> 137 us; a layer of them alone (155 MB), again and again, 32.3 -> 34.4.
+static int nt_pages(const CacheDev &c, int B) {
+  const size_t page = (size_t)c.L * B * c.KV * 2 * CACHE_BLOCK * c.dh;
+  return (int)std::min<size_t>((((size_t)384 << 20) + page - 1) / page, INT32_MAX);
+}
+
 int cache_split_target(const CacheDev &c, int B, int P) {
   const long per = (long)c.KV * call_groups(c, P), full = CACHE_SPLIT_WAVES / waves_of(c, B, P);
   return per > full || B * per > CACHE_JOINS ? 0 : (int)(full / per);
@@ -725,6 +748,7 @@ void launch_cache_attend(const CacheDev &c, const CacheAttend &call, hipStream_t
   const int waves = waves_of(c, a.B, a.P);
   const int target = cache_split_target(c, a.B, a.P), items = a.B + (target ? 3 * target + 1 : 0);
   a.whole = target == 0;
+  a.nt_pages = nt_pages(c, a.B);
   if (!one) launch_cache_append(c, a.layer, a.B, a.P, a.kv, st);
   auto go = [&](auto act, auto width) {
     typedef decltype(act) ACT;
@@ -733,13 +757,23 @@ void launch_cache_attend(const CacheDev &c, const CacheAttend &call, hipStream_t
       constexpr int MT = decltype(mt)::value;
       constexpr bool ONE = decltype(is_one)::value;
       const dim3 grid(items, c.KV, call_groups(c, a.P));
-      if constexpr (eight_fit(DH, sizeof(ACT) == 2, MT, ONE)) {
-        if (waves == 8) {
-          hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 8, ONE>), grid, dim3(512), 0, st, ev0, ev1, 0, c, a);
+      auto with = [&](auto nt) {
+        constexpr bool HINT = decltype(nt)::value;
+        if constexpr (eight_fit(DH, sizeof(ACT) == 2, MT, ONE)) {
+          if (waves == 8) {
+            hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 8, ONE, HINT>), grid, dim3(512), 0, st, ev0, ev1, 0, c, a);
+            return;
+          }
+        }
+        hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 4, ONE, HINT>), grid, dim3(256), 0, st, ev0, ev1, 0, c, a);
+      };
+      if constexpr (ONE && sizeof(ACT) == 2) {   // (groups of a row share its pages; fp32 rows are bound by other things)
+        if (c.NP > a.nt_pages) {
+          with(std::true_type{});
           return;
         }
       }
-      hipExtLaunchKernelGGL((k_cache_attend<ACT, DH, MT, 4, ONE>), grid, dim3(256), 0, st, ev0, ev1, 0, c, a);
+      with(std::false_type{});
     };
     constexpr int MOST = max_tiles(DH, sizeof(ACT) == 2);
     const int mt = tiles_of(c, R);
