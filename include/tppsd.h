@@ -75,8 +75,8 @@ extern "C" {
 #define TPPSD_STATUS_AR_CAP    4u  /* Theorem-1 loop hit TPPSD_AR_ITER_CAP        */
 #define TPPSD_STATUS_PAGES     8u  /* cache: no free page for a row; it was left out */
 #define TPPSD_STATUS_SEQUENCE 16u  /* cache: a sequence that does not exist, or named twice */
-#define TPPSD_STATUS_OPEN     32u  /* cache: a length inside a block whose rows are no longer held;
-                                      rounded down to the block */
+#define TPPSD_STATUS_OPEN     32u  /* cache: a length inside a block whose rows are no longer held
+                                      (commit, truncate: rounded down to the block) */
 
 #define TPPSD_AR_ITER_CAP (1 << 20)
 
@@ -461,7 +461,10 @@ int tppsd_cache_reset(tppsd_cache *c, hipStream_t stream);
  * sequence does not exist or an earlier row names it (TPPSD_STATUS_SEQUENCE),
  * when it would pass max_events (TPPSD_STATUS_CAPACITY), or when the pages that
  * it and the rows before it need are not there (TPPSD_STATUS_PAGES). A plan that
- * was not committed is dropped. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no reset),
+ * was not committed is dropped; if it appended more than 64 positions, the rows
+ * of a sequence's open block may have made way for the last ones, and the next
+ * call of that sequence sets TPPSD_STATUS_OPEN (commit such calls, with 0
+ * positions if need be, or truncate the sequence to its whole blocks). Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no reset),
  * TPPSD_E_HIP. */
 int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, const int32_t *d_counts,
                       hipStream_t stream);

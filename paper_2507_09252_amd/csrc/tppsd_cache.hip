@@ -114,6 +114,11 @@ __device__ __forceinline__ void pages_drop(const CacheDev &c, int s, int j0, int
   if (low < seen) atomicMin(&c.counts[2], low);
 }
 
+// whether a sequence of n positions has an open block that the ring (from block
+// `low` on) no longer holds: a call of more than two blocks that was dropped has
+// taken its place
+__device__ __forceinline__ bool open_lost(int n, int low) { return n % CACHE_BLOCK != 0 && n / CACHE_BLOCK < low; }
+
 __global__ void k_cache_reset(CacheDev c) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
   for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
@@ -227,7 +232,11 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
         off += need;
       }
       c.pend[r.seq] = r.cnt;
-      if (r.cnt > 0) c.low[r.seq] = max(top_of(r) - 1, min(c.low[r.seq], r.start / CACHE_BLOCK));
+      if (r.cnt > 0) {
+        const int low = c.low[r.seq];
+        if (open_lost(r.start, low)) atomicOr(c.status, TPPSD_STATUS_OPEN);
+        c.low[r.seq] = max(top_of(r) - 1, min(low, r.start / CACHE_BLOCK));
+      }
     }
     if (PER > 0) c.p_seq[i] = r.seq, c.p_start[i] = r.start, c.p_count[i] = r.cnt;
     mine.b += top_of(r);
@@ -277,7 +286,7 @@ __global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
   const int s = c.p_seq[i], cnt = c.p_count[i];
   if (s < 0 || cnt <= 0) return;
   int n = c.p_start[i] + (accept ? min(max(accept[i], 0), cnt) : cnt);
-  if (n % CACHE_BLOCK && n / CACHE_BLOCK < c.low[s]) {   // the ring no longer holds the block that would be open
+  if (open_lost(n, c.low[s])) {
     atomicOr(c.status, TPPSD_STATUS_OPEN);
     n = n / CACHE_BLOCK * CACHE_BLOCK;
   }
@@ -297,7 +306,7 @@ __global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t 
       const int len = ld_agent(&c.lens[s]);
       if (n >= len) {
         n = len;
-      } else if (n % CACHE_BLOCK && n / CACHE_BLOCK < c.low[s]) {
+      } else if (open_lost(n, c.low[s])) {
         atomicOr(c.status, TPPSD_STATUS_OPEN);
         n = n / CACHE_BLOCK * CACHE_BLOCK;
       }
@@ -428,6 +437,7 @@ __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int
     c.table[(size_t)d * c.NP + j] = page;
   }
   if (threadIdx.x == 0) {
+    if (open_lost(len, c.low[s])) atomicOr(c.status, TPPSD_STATUS_OPEN);
     c.lens[d] = len;
     c.held[d] = np;
     c.low[d] = np;
@@ -496,6 +506,7 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
         atomicAdd(&to.refs[page], 1);
       }
       if (threadIdx.x == 0) {
+        if (open_lost(len, from.low[s])) atomicOr(to.status, TPPSD_STATUS_OPEN);
         to.lens[d] = len;
         to.held[d] = to.low[d] = np;
       }

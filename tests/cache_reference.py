@@ -65,6 +65,8 @@ class CacheRef:
                 off += need
             self.pend[s] = cnt
             if cnt:
+                if start % BLOCK and start // BLOCK < self.low[s]:
+                    self.status |= OPEN
                 top = (start + cnt - 1) // BLOCK
                 self.low[s] = max(top - 1, min(self.low[s], start // BLOCK))
             self.plan.append((s, start, cnt))
@@ -153,6 +155,8 @@ class CacheRef:
 
     def _take(self, d, other, s):
         n = int(other.lens[s])
+        if n % BLOCK and n // BLOCK < other.low[s]:
+            self.status |= OPEN
         self.rows[d, :, :, :n] = other.rows[s, :, :, :n]
         self.lens[d], self.held[d], self.low[d], self.pend[d] = n, n // BLOCK, n // BLOCK, 0
 

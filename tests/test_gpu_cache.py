@@ -529,3 +529,58 @@ def test_long_lists_of_pairs(n, S):
     o.step(queries=False)
     o.commit()
     o.same()
+
+
+def test_dropped_calls():
+    """A plan that is not committed: short calls leave the sequence as it was;
+    longer ones may take the open block's rows, which the status tells."""
+    b = Both(1, 2, 2, 32, "bf16", 4, 500, seed=21)
+    b.begin(100, counts=[100, 64, 100, 0])
+    b.step(queries=False)
+    b.commit()
+    for P in (64, 5, 33):
+        b.begin(P)
+        b.step(queries=False)
+    b.begin(20)
+    b.step()                                    # (compared with what a single call gives)
+    b.commit([7, 20, 0, 3])
+    b.same(0)
+    b.begin(200, counts=[0, 200, 200, 200])     # sequence 1 began inside a block, 2 too
+    b.step(queries=False)
+    b.begin(4, seqs=[0])
+    b.step()
+    b.commit()
+    assert b.c.tppsd_cache_status() == 0
+    b.begin(4, seqs=[1])
+    assert b.c.tppsd_cache_status() == OPEN == b.r.status
+    b.c.tppsd_cache_truncate(ints([1, 2, 3]), ints([64, 64, 0]))
+    b.r.truncate([1, 2, 3], [64, 64, 0])
+    b.begin(70)
+    b.step()
+    b.commit()
+    b.same(OPEN)
+
+
+def test_forks_in_a_captured_graph():
+    """Truncation, forks and copies captured and replayed: the same as when called."""
+    b, o = Both(2, 1, 1, 32, "bf16", 5, 300, seed=1), tp.Cache(2, 1, 1, 32, "bf16", 5, 300)
+    b.begin(200, counts=[200, 150, 70, 10, 0])
+    b.step(queries=False)
+    b.commit()
+    src, dst, cut, lens, every = ints([0, 0]), ints([3, 4]), ints([1, 2]), ints([128, 64]), ints(range(5))
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        b.c.tppsd_cache_fork(src, dst)
+        b.c.tppsd_cache_truncate(cut, lens)
+        o.tppsd_cache_copy(b.c, every, every)
+    torch.cuda.current_stream().wait_stream(side)
+    b.r.fork([0, 0], [3, 4])
+    b.r.truncate([1, 2], [128, 64])
+    for _ in range(3):
+        graph.replay()
+        b.same(0)
+        assert torch.equal(o.lens, b.c.lens) and o.tppsd_cache_status() == 0
+        for layer in range(2):
+            for x, y in zip(o.tppsd_cache_read(layer, None, 200), b.c.tppsd_cache_read(layer, None, 200)):
+                assert torch.equal(x, y)
