@@ -502,7 +502,7 @@ int forward(tppsd_state *s, const tppsd_model *m, const ModelCache &c, const int
     b.P = P;
     b.start_in = start;
     b.start_off = start_off;
-    b.done = s->done;
+    b.done = head ? s->done : nullptr;   // (a history is encoded whole, also where nothing follows it)
     b.split_target = cache_split_target(s->c8, B, P);
     launch_cache_begin(s->c8, b, st);
   }

@@ -119,6 +119,10 @@ __device__ __forceinline__ void pages_drop(const CacheDev &c, int s, int j0, int
 // taken its place
 __device__ __forceinline__ bool open_lost(int n, int low) { return n % CACHE_BLOCK != 0 && n / CACHE_BLOCK < low; }
 
+// whole pages that a sequence of n positions has to share or copy: never more than it holds
+// (entries of the table behind those are -1)
+__device__ __forceinline__ int pages_of(const CacheDev &c, int s, int n) { return min(n / CACHE_BLOCK, c.held[s]); }
+
 __global__ void k_cache_reset(CacheDev c) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
   for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
@@ -424,7 +428,7 @@ __device__ void copy_tail(const CacheDev &to, const CacheDev &from, int l0, int 
 __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int32_t *src, const int32_t *dst) {
   const int i = blockIdx.x;
   if (!pair_goes(c, c, n, src, dst, i, true)) return;
-  const int s = src[i], d = dst[i], len = c.lens[s], np = len / CACHE_BLOCK;
+  const int s = src[i], d = dst[i], len = c.lens[s], np = pages_of(c, s, len);
   if (blockIdx.y > 0) {
     copy_tail(c, c, blockIdx.y - 1, gridDim.y - 1, s, d, len);
     return;
@@ -456,7 +460,7 @@ __global__ __launch_bounds__(256) void k_copy_mark(CacheDev to, CacheDev from, i
   }
   if (threadIdx.x == 0) to.p_seq[i] = go ? 1 : 0;
   if (!go) return;
-  const int np = from.lens[s] / CACHE_BLOCK;
+  const int np = pages_of(from, s, from.lens[s]);
   for (int j = threadIdx.x; j < np; j += blockDim.x) {
     const int page = from.table[(size_t)s * from.NP + j];
     atomicOr(&from.mark[page >> 5], 1u << (page & 31));
@@ -496,7 +500,7 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
   if ((int)blockIdx.x < seq_wgs) {
     const int i = blockIdx.x % n, y = (int)blockIdx.x / n;
     if (!to.p_seq[i]) return;
-    const int s = src[i], d = dst[i], len = from.lens[s], np = len / CACHE_BLOCK;
+    const int s = src[i], d = dst[i], len = from.lens[s], np = pages_of(from, s, len);
     if (y > 0) {
       copy_tail(to, from, y - 1, Y - 1, s, d, len);
     } else {

@@ -273,3 +273,30 @@ def test_fork_refusals():
     assert s["bits"] == tp.STATUS_SEQUENCE and s["n_done"] == 2
     b.tppsd_sample_sd(4)
     assert b.tppsd_read_events()[2].tolist() == [50, 0, 0]
+
+
+@pytest.mark.parametrize("cache8", [False, True])
+def test_poisson_and_windowed_jobs_fork(cache8):
+    """States without a draft model, and with end times: forks take both along."""
+    c = case("c2", 3, 70)
+    wt, wd = weights(c)
+    ht, hk = (to_dev(x) for x in histories(c))
+    params = tp.tppsd_poisson_fit(ht, hk, c.wl.target.n_types)
+    a = state(c, wt, wd, 4, 30, 5, draft=False, cache8=cache8)
+    a.tppsd_prefill(ht, hk, 30)
+    a.tppsd_sample_sd_poisson(4, params, 2)
+    b = state(c, wt, wd, 4, 30, 5, cache8=cache8, models=a._models, extra=9)
+    b.tppsd_state_fork(a, torch.arange(3, device="cuda"))
+    for st in (a, b):
+        st.tppsd_sample_sd_poisson(4, params)
+    assert torch.equal(a.tppsd_read_events()[0][:, :100], b.tppsd_read_events()[0][:, :100])
+    end = ht[:, -1] + torch.tensor([0.0, 5.0, 1e6], device="cuda")
+    a = state(c, wt, wd, 4, 30, 5, cache8=cache8)
+    a.tppsd_prefill(ht, hk, 30, t_end=end)
+    b = state(c, wt, wd, 4, 30, 5, cache8=cache8, models=a._models)
+    b.tppsd_state_fork(a, torch.tensor([2, 1, 0], device="cuda"))
+    assert b.tppsd_state_status()["n_done"] == 1
+    b.tppsd_sample_sd(4)
+    t, _, n = b.tppsd_read_events()
+    assert n[2] == 70 and n[0] == 100 and t[1, int(n[1]) - 1] <= end[1]
+    assert b.tppsd_state_status()["bits"] == 0
