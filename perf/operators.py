@@ -193,7 +193,6 @@ def prepare(case, seed):
         par = case["parents"]
         s["src"] = _ints([i % par for i in range(B - par)])
         s["dst"] = _ints(list(range(par, B)))
-        s["shape"] = (max(lens) // BLOCK or 1, sum(n // BLOCK for n in lens) or 1)
     if own:
         from paper_2507_09252_amd import tppsd as tp
         c = tp.Cache(L, case["heads"], KV, dh, case["prec"], B, max(lens) + P + BLOCK)
@@ -447,8 +446,10 @@ def _own_append(s):
 
 
 def _own_fork(s):
-    c, (pages, used) = s["cache"], s["shape"]
+    c = s["cache"]
     c.tppsd_cache_fork(s["src"], s["dst"])
+    pages = (max(_lens(s["case"])) // BLOCK) or 1
+    used = sum(n // BLOCK for n in _lens(s["case"])) or 1
     return {"table": c.table[:, :pages], "lens": c.lens, "refs": c.refs[:used], "tails": c.tails}
 
 
