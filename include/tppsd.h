@@ -460,12 +460,19 @@ int tppsd_cache_reset(tppsd_cache *c, hipStream_t stream);
  * left out (nothing appended, its output rows left as they were) when its
  * sequence does not exist or an earlier row names it (TPPSD_STATUS_SEQUENCE),
  * when it would pass max_events (TPPSD_STATUS_CAPACITY), or when the pages that
- * it and the rows before it need are not there (TPPSD_STATUS_PAGES). A plan that
- * was not committed is dropped; if it appended more than 64 positions, the rows
- * of a sequence's open block may have made way for the last ones, and the next
- * call of that sequence sets TPPSD_STATUS_OPEN (commit such calls, with 0
- * positions if need be, or truncate the sequence to its whole blocks). Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no reset),
- * TPPSD_E_HIP. */
+ * it and the rows before it need are not there (TPPSD_STATUS_PAGES). Pages of
+ * positions that do not stay are the sequence's until it gets there or is truncated.
+ *
+ * A plan that was not committed is dropped. If it appended more than 64
+ * positions, the rows of a sequence's open block may have made way for the last
+ * ones. Such a block is lost: every call of the sequence sets TPPSD_STATUS_OPEN,
+ * its positions see in the block's place what its slots hold now, and its commit
+ * keeps none of them and takes the sequence back to its whole blocks; forks and
+ * copies of the sequence are of its whole blocks. So commit long calls, or
+ * truncate the sequences of a dropped one to whole blocks.
+ *
+ * A captured graph holds a call's begin together with its layers. Errors:
+ * TPPSD_E_ARG, TPPSD_E_ORDER (no reset), TPPSD_E_HIP. */
 int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, const int32_t *d_counts,
                       hipStream_t stream);
 
@@ -487,7 +494,8 @@ int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
 /* Ends the call: row i keeps the first d_accept[i] of its positions (clamped to
  * 0..its count; NULL: all). What is dropped may be brought again. After a call of
  * more than 64 positions a length inside a block before the last two is rounded
- * down to that block (TPPSD_STATUS_OPEN). Errors: TPPSD_E_ORDER, TPPSD_E_HIP. */
+ * down to that block, and a sequence whose open block was lost before the call
+ * goes back to its whole blocks (TPPSD_STATUS_OPEN). Errors: TPPSD_E_ORDER, TPPSD_E_HIP. */
 int tppsd_cache_commit(tppsd_cache *c, const int32_t *d_accept, hipStream_t stream);
 
 /* Shortens sequences d_seqs[0 .. n) to d_lens (NULL: 0; a length at or past a
@@ -500,7 +508,7 @@ int tppsd_cache_truncate(tppsd_cache *c, int n, const int32_t *d_seqs, const int
 
 /* d_dst[j] becomes a copy of sequence d_src[j], j < n <= max_seqs: what it held is freed,
  * whole pages are shared (they are never written again) and the open block's
- * rows copied. A source may be named many times; a pair whose destination
+ * rows copied (TPPSD_STATUS_OPEN: not those of a lost block). A source may be named many times; a pair whose destination
  * another pair names before it or as a source is left out
  * (TPPSD_STATUS_SEQUENCE); a pair of two negative numbers is none. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
 int tppsd_cache_fork(tppsd_cache *c, int n, const int32_t *d_src, const int32_t *d_dst, hipStream_t stream);

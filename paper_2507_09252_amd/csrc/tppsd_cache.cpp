@@ -75,6 +75,7 @@ size_t view(CacheDev *c, char *ws, Entry *entries) {
   take(c->refs, N * 4, "refs");
   take(c->held, S * 4);
   take(c->low, S * 4);
+  take(c->lost, S * 4);
   take(c->pend, S * 4);
   take(c->freeb, (N + 31) / 32 * 4);
   take(c->owner, S * 4);

@@ -46,6 +46,7 @@ struct CacheDev {
   int32_t *refs;      // [n_pages] sequences that hold the page
   int32_t *held;      // [S] pages held (those of uncommitted blocks too)
   int32_t *low;       // [S] first block whose rows the ring holds
+  int32_t *lost;      // [S] the plan's positions follow an open block that is not in the ring any more
   int32_t *pend;      // [S] positions appended and not committed
   uint32_t *freeb;    // [ceil(n_pages / 32)] bit set: page is free
   int32_t *owner;     // [S] scratch: which row of a call names the sequence

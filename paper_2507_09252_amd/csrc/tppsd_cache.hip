@@ -114,10 +114,18 @@ __device__ __forceinline__ void pages_drop(const CacheDev &c, int s, int j0, int
   if (low < seen) atomicMin(&c.counts[2], low);
 }
 
-// whether a sequence of n positions has an open block that the ring (from block
+// Whether a sequence of n positions has an open block that the ring (from block
 // `low` on) no longer holds: a call of more than two blocks that was dropped has
-// taken its place
+// taken its place. Until the sequence ends at a block's border again `low` only
+// rises, so that nothing takes the slots' rows for that block's.
 __device__ __forceinline__ bool open_lost(int n, int low) { return n % CACHE_BLOCK != 0 && n / CACHE_BLOCK < low; }
+
+// Positions of a sequence that another can take over: without the open block
+// where that is lost.
+__device__ __forceinline__ int sound_len(const CacheDev &c, int s) {
+  const int n = c.lens[s];
+  return open_lost(n, c.low[s]) ? n / CACHE_BLOCK * CACHE_BLOCK : n;
+}
 
 // whole pages that a sequence of n positions has to share or copy: never more than it holds
 // (entries of the table behind those are -1)
@@ -126,7 +134,7 @@ __device__ __forceinline__ int pages_of(const CacheDev &c, int s, int n) { retur
 __global__ void k_cache_reset(CacheDev c) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
   for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
-  for (size_t j = i; j < (size_t)c.S; j += n) c.lens[j] = c.held[j] = c.low[j] = c.pend[j] = 0;
+  for (size_t j = i; j < (size_t)c.S; j += n) c.lens[j] = c.held[j] = c.low[j] = c.lost[j] = c.pend[j] = 0;
   for (size_t j = i; j < (size_t)c.n_pages; j += n) c.refs[j] = 0;
   for (size_t j = i; j < (size_t)(c.n_pages + 31) / 32; j += n) {
     const int left = c.n_pages - (int)j * 32;
@@ -238,8 +246,10 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
       c.pend[r.seq] = r.cnt;
       if (r.cnt > 0) {
         const int low = c.low[r.seq];
-        if (open_lost(r.start, low)) atomicOr(c.status, TPPSD_STATUS_OPEN);
-        c.low[r.seq] = max(top_of(r) - 1, min(low, r.start / CACHE_BLOCK));
+        const bool lost = open_lost(r.start, low);
+        if (lost) atomicOr(c.status, TPPSD_STATUS_OPEN);
+        c.lost[r.seq] = lost;
+        c.low[r.seq] = max(top_of(r) - 1, lost ? low : min(low, r.start / CACHE_BLOCK));
       }
     }
     if (PER > 0) c.p_seq[i] = r.seq, c.p_start[i] = r.start, c.p_count[i] = r.cnt;
@@ -290,6 +300,7 @@ __global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
   const int s = c.p_seq[i], cnt = c.p_count[i];
   if (s < 0 || cnt <= 0) return;
   int n = c.p_start[i] + (accept ? min(max(accept[i], 0), cnt) : cnt);
+  if (c.lost[s]) n = c.p_start[i];   // (rows behind a lost block are no good either)
   if (open_lost(n, c.low[s])) {
     atomicOr(c.status, TPPSD_STATUS_OPEN);
     n = n / CACHE_BLOCK * CACHE_BLOCK;
@@ -428,7 +439,7 @@ __device__ void copy_tail(const CacheDev &to, const CacheDev &from, int l0, int 
 __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int32_t *src, const int32_t *dst) {
   const int i = blockIdx.x;
   if (!pair_goes(c, c, n, src, dst, i, true)) return;
-  const int s = src[i], d = dst[i], len = c.lens[s], np = pages_of(c, s, len);
+  const int s = src[i], d = dst[i], len = sound_len(c, s), np = pages_of(c, s, len);
   if (blockIdx.y > 0) {
     copy_tail(c, c, blockIdx.y - 1, gridDim.y - 1, s, d, len);
     return;
@@ -441,7 +452,7 @@ __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int
     c.table[(size_t)d * c.NP + j] = page;
   }
   if (threadIdx.x == 0) {
-    if (open_lost(len, c.low[s])) atomicOr(c.status, TPPSD_STATUS_OPEN);
+    if (len < c.lens[s]) atomicOr(c.status, TPPSD_STATUS_OPEN);
     c.lens[d] = len;
     c.held[d] = np;
     c.low[d] = np;
@@ -454,13 +465,13 @@ __global__ __launch_bounds__(256) void k_copy_mark(CacheDev to, CacheDev from, i
                                                    const int32_t *dst) {
   const int i = blockIdx.x, s = src[i], d = dst[i];
   bool go = pair_goes(to, from, n, src, dst, i, false);
-  if (go && from.lens[s] > to.max_events) {
+  if (go && sound_len(from, s) > to.max_events) {
     if (threadIdx.x == 0) atomicOr(to.status, TPPSD_STATUS_CAPACITY);
     go = false;
   }
   if (threadIdx.x == 0) to.p_seq[i] = go ? 1 : 0;
   if (!go) return;
-  const int np = pages_of(from, s, from.lens[s]);
+  const int np = pages_of(from, s, sound_len(from, s));
   for (int j = threadIdx.x; j < np; j += blockDim.x) {
     const int page = from.table[(size_t)s * from.NP + j];
     atomicOr(&from.mark[page >> 5], 1u << (page & 31));
@@ -500,7 +511,7 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
   if ((int)blockIdx.x < seq_wgs) {
     const int i = blockIdx.x % n, y = (int)blockIdx.x / n;
     if (!to.p_seq[i]) return;
-    const int s = src[i], d = dst[i], len = from.lens[s], np = pages_of(from, s, len);
+    const int s = src[i], d = dst[i], len = sound_len(from, s), np = pages_of(from, s, len);
     if (y > 0) {
       copy_tail(to, from, y - 1, Y - 1, s, d, len);
     } else {
@@ -510,7 +521,7 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
         atomicAdd(&to.refs[page], 1);
       }
       if (threadIdx.x == 0) {
-        if (open_lost(len, from.low[s])) atomicOr(to.status, TPPSD_STATUS_OPEN);
+        if (len < from.lens[s]) atomicOr(to.status, TPPSD_STATUS_OPEN);
         to.lens[d] = len;
         to.held[d] = to.low[d] = np;
       }
