@@ -99,6 +99,16 @@ __device__ __forceinline__ uint32_t bf_bad(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
 
+// 8 elements of a key with its infinities as NaN: a product of infinity with an
+// element of the other sign would be a score of -inf, a weight of 0, and the key
+// as good as masked. (fp32 keys have it from their parts: inf - inf.)
+__device__ __forceinline__ Eight<bf16_t> nan_keys(Eight<bf16_t> k) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k.w[0][i] |= bf_bad(k.w[0][i]) & 0x00400040u;
+  return k;
+}
+__device__ __forceinline__ Eight<float> nan_keys(const Eight<float> &k) { return k; }
+
 // The operand of 8 values of a column, four at p and four at p + 16, in parts;
 // clean: those that are not finite as 0, or (bad) 1 in their place and 0 elsewhere.
 template <int NP> __device__ __forceinline__ void value8(const bf16_t *p, bool clean, bf16x8_t (&v)[NP]) {
@@ -491,7 +501,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
       } else {
         vv.load(vp);
       }
-      kk.store(&win.k[row][j]);
+      nan_keys(kk).store(&win.k[row][j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const ACT v = in ? vv.at(e) : (ACT)0, k = kk.at(e);
