@@ -526,9 +526,10 @@ int tppsd_cache_copy(tppsd_cache *to, tppsd_cache *from, int n, const int32_t *d
                      hipStream_t stream);
 
 /* Rows of positions d_first[i] (NULL: 0) .. + count - 1 of sequences d_seqs[i]
- * (NULL: i) as the cache holds them, appended and not yet committed ones
- * included, into d_k and d_v [n, count, n_kv_heads, d_head]; rows past a sequence's end are
- * left as they were. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+ * (NULL: i) as the cache holds them, into d_k and d_v [n, count, n_kv_heads,
+ * d_head]: the committed ones, and those of the call in progress once this layer
+ * has appended them. Rows past a sequence's end, and those of a lost open block
+ * (TPPSD_STATUS_OPEN), are left as they were. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
 int tppsd_cache_read(tppsd_cache *c, int layer, int n, const int32_t *d_seqs, const int32_t *d_first, int count,
                      void *d_k, void *d_v, hipStream_t stream);
 

@@ -77,6 +77,8 @@ size_t view(CacheDev *c, char *ws, Entry *entries) {
   take(c->low, S * 4);
   take(c->lost, S * 4);
   take(c->pend, S * 4);
+  take(c->planned, S * 4);
+  take(c->came, L * S * 4);
   take(c->freeb, (N + 31) / 32 * 4);
   take(c->owner, S * 4);
   take(c->role, S * 4);

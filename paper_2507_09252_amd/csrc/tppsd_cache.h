@@ -47,14 +47,17 @@ struct CacheDev {
   int32_t *held;      // [S] pages held (those of uncommitted blocks too)
   int32_t *low;       // [S] first block whose rows the ring holds
   int32_t *lost;      // [S] the plan's positions follow an open block that is not in the ring any more
-  int32_t *pend;      // [S] positions appended and not committed
+  int32_t *pend;      // [S] positions that the plan brings and that are not committed
+  int32_t *planned;   // [S] number of the last plan that brings the sequence any
+  int32_t *came;      // [L][S] number of the last plan whose rows the layer has
   uint32_t *freeb;    // [ceil(n_pages / 32)] bit set: page is free
   int32_t *owner;     // [S] scratch: which row of a call names the sequence
   int32_t *role;      // [S] scratch of forks
   int32_t *list;      // [n_pages] scratch: pages in the order of a scan
   int32_t *map;       // [n_pages] scratch of copies: destination page
   uint32_t *mark;     // [ceil(n_pages / 32)] scratch of copies: pages to copy
-  int32_t *counts;    // [8] items of the plan, pages to copy, a word of freeb before which no page is free
+  int32_t *counts;    // [8] items of the plan, pages to copy, a word of freeb before which no page is free,
+                      // number of the plan (calls that drop a plan take one too)
   // plan of the call in progress, one row per sequence of the batch
   int32_t *p_seq, *p_start, *p_count;   // [S]
   CacheItem *items;

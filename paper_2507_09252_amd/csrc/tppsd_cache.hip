@@ -134,7 +134,9 @@ __device__ __forceinline__ int pages_of(const CacheDev &c, int s, int n) { retur
 __global__ void k_cache_reset(CacheDev c) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
   for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
-  for (size_t j = i; j < (size_t)c.S; j += n) c.lens[j] = c.held[j] = c.low[j] = c.lost[j] = c.pend[j] = 0;
+  for (size_t j = i; j < (size_t)c.S; j += n)
+    c.lens[j] = c.held[j] = c.low[j] = c.lost[j] = c.pend[j] = c.planned[j] = 0;
+  for (size_t j = i; j < (size_t)c.L * c.S; j += n) c.came[j] = 0;
   for (size_t j = i; j < (size_t)c.n_pages; j += n) c.refs[j] = 0;
   for (size_t j = i; j < (size_t)(c.n_pages + 31) / 32; j += n) {
     const int left = c.n_pages - (int)j * 32;
@@ -145,8 +147,12 @@ __global__ void k_cache_reset(CacheDev c) {
   if (i == 0) {
     *c.status = 0u;
     c.counts[2] = 0;
+    c.counts[PLAN_ID] = 0;
   }
 }
+
+// a plan in progress is dropped: what it brought is nobody's
+__device__ __forceinline__ void drop_plan(const CacheDev &c) { c.counts[PLAN_ID] += 1; }
 
 // Plans a call: which sequence each row of the batch names, its first new
 // position and how many it brings; pages for the blocks that become whole; and
@@ -196,7 +202,7 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
   }
   auto top_of = [&](const Row &r) { return r.cnt > 0 ? (r.start + r.cnt - 1) / CACHE_BLOCK : 0; };
   auto need_of = [&](const Row &r) { return r.cnt > 0 ? max(0, (r.start + r.cnt) / CACHE_BLOCK - r.held) : 0; };
-  const int hint = c.counts[2];
+  const int hint = c.counts[2], plan = c.counts[PLAN_ID] + 1;
   Sums mine = {0, 0, 0}, before;
   each(true, [&](int i, Row &r) {
     const int s = b.seqs ? b.seqs[i] : i;
@@ -249,6 +255,7 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
         const bool lost = open_lost(r.start, low);
         if (lost) atomicOr(c.status, TPPSD_STATUS_OPEN);
         c.lost[r.seq] = lost;
+        c.planned[r.seq] = plan;
         c.low[r.seq] = max(top_of(r) - 1, lost ? low : min(low, r.start / CACHE_BLOCK));
       }
     }
@@ -256,6 +263,7 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
     mine.b += top_of(r);
     mine.top = max(mine.top, top_of(r));
   });
+  if (tid == 0) c.counts[PLAN_ID] = plan;
   if (avail < all.a && b.split_target > 0) all = block_sums(mine, &before, sums);   // (rows were left out)
   // Work items. Rows of about equal length that fill the chip are taken whole.
   // Otherwise pages are dealt out in pieces of a workgroup's share, or, where
@@ -306,12 +314,13 @@ __global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
     n = n / CACHE_BLOCK * CACHE_BLOCK;
   }
   c.lens[s] = n;
-  c.pend[s] = 0;
+  c.pend[s] = c.lost[s] = 0;
 }
 
 __global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t *lens) {
   __shared__ int range[2];
   const int s = seqs[blockIdx.x];
+  if (blockIdx.x == 0 && threadIdx.x == 0) drop_plan(c);
   if (threadIdx.x == 0) {
     range[0] = range[1] = 0;
     int n = lens ? lens[blockIdx.x] : 0;
@@ -438,6 +447,7 @@ __device__ void copy_tail(const CacheDev &to, const CacheDev &from, int l0, int 
 // 142 MB: 35 us).
 __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int32_t *src, const int32_t *dst) {
   const int i = blockIdx.x;
+  if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) drop_plan(c);
   if (!pair_goes(c, c, n, src, dst, i, true)) return;
   const int s = src[i], d = dst[i], len = sound_len(c, s), np = pages_of(c, s, len);
   if (blockIdx.y > 0) {
@@ -495,6 +505,7 @@ __global__ __launch_bounds__(PLAN_NT) void k_copy_plan(CacheDev to, CacheDev fro
   }
   for (int w = threadIdx.x; w < (from.n_pages + 31) / 32; w += PLAN_NT) from.mark[w] = 0u;
   if (threadIdx.x == 0) {
+    drop_plan(to);
     to.counts[1] = fits ? n : -1;
     if (fits && n > 0) to.counts[2] = to.list[n - 1] >> 5;
     if (!fits) atomicOr(to.status, TPPSD_STATUS_PAGES);
@@ -555,7 +566,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int
   __shared__ __align__(16) ACT vs[DH][LDV];            // values, row per column
   __shared__ float top[2][4];
   const int i = blockIdx.x, h = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int s = c.p_seq[i], cnt = c.p_count[i], start = c.p_start[i];
+  const int s = c.p_seq[i], cnt = c.p_count[i], start = c.p_start[i], plan = c.counts[PLAN_ID];
   if (s < 0 || cnt <= 0) return;
   const int end = start + cnt, first = start / CACHE_BLOCK, last = (end - 1) / CACHE_BLOCK;
   const int blk = first + blockIdx.z;
@@ -628,6 +639,7 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int
       v2.store(ring + (CACHE_RING + pos % CACHE_RING) * DH + j);
     }
   }
+  if (blk == first && h == 0 && tid == 0) c.came[(size_t)layer * c.S + s] = plan;
   if (!whole) return;
   top_k = lanes_max(top_k);
   top_v = lanes_max(top_v);
@@ -639,7 +651,9 @@ __global__ __launch_bounds__(256) void k_cache_append(CacheDev c, int layer, int
 
 // Rows first[i] .. first[i] + count - 1 of sequences, as the cache holds them:
 // whole blocks from their codes, through LDS, the open block from the ring;
-// positions past the sequence are left as they were. Grid (row, head, block).
+// positions past the sequence are left as they were. A plan's positions are the
+// sequence's once the layer has them and while the plan stands; a lost open
+// block is not (but for the plan that follows it). Grid (row, head, block).
 // Bound by memory (the histories above in 48 us).
 template <typename ACT, int DH>
 __global__ __launch_bounds__(256) void k_cache_read(CacheDev c, int layer, const int32_t *seqs, const int32_t *first,
@@ -652,12 +666,20 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheDev c, int layer, const
     if (tid == 0) atomicOr(c.status, TPPSD_STATUS_SEQUENCE);
     return;
   }
-  const int end = c.lens[s] + c.pend[s], blk = f / CACHE_BLOCK + blockIdx.z, base = blk * CACHE_BLOCK;
+  const int blk = f / CACHE_BLOCK + blockIdx.z, base = blk * CACHE_BLOCK;
+  const int page_id = c.table[(size_t)s * c.NP + min(blk, c.NP - 1)];   // (with the loads below)
+  const int len = c.lens[s], pend = c.pend[s], plan = c.counts[PLAN_ID];
+  const bool has = c.came[(size_t)layer * c.S + s] == plan;
+  int end = has ? len + pend : len;
+  if (!has && (c.planned[s] == plan ? c.lost[s] != 0 : open_lost(len, c.low[s]))) {
+    if (tid == 0) atomicOr(c.status, TPPSD_STATUS_OPEN);
+    end = len / CACHE_BLOCK * CACHE_BLOCK;
+  }
   const int lo = max(f, base), hi = min(base + CACHE_BLOCK, f > end ? f : min(end, count > end - f ? end : f + count));
   if (lo >= hi) return;
   const bool whole = base + CACHE_BLOCK <= end;
   if (whole) {
-    const size_t tile = ((size_t)layer * c.n_pages + c.table[(size_t)s * c.NP + blk]) * c.KV + h;
+    const size_t tile = ((size_t)layer * c.n_pages + page_id) * c.KV + h;
     const u32x4_t *page = (const u32x4_t *)(c.pages + tile * (2 * CACHE_BLOCK * DH));
     const float sk = c.scales[tile * 2], sv = c.scales[tile * 2 + 1];
     for (int x = tid; x < CACHE_BLOCK * DH / 8; x += 256)

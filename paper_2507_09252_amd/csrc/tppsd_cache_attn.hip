@@ -515,6 +515,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
         vv.store(to + CACHE_RING * DH);
       }
     }
+    if (ONE && h == 0 && tid == 0) c.came[(size_t)a.layer * c.S + seq] = c.counts[PLAN_ID];
     any_bad = __syncthreads_or(bad);
     if constexpr (ONE) {
       if (n >= CACHE_BLOCK) {   // the first block is whole: its page

@@ -6,6 +6,8 @@
 
 namespace tppsd {
 
+constexpr int PLAN_ID = 3;   // counts: number of the plan
+
 // ---- fragment order ---------------------------------------------------------
 // A (page, layer, head) tile is the keys' 64 dh codes, then the values'. The
 // attention reads both in 16-byte words, word c of lane l = 16 g + m at

@@ -1,5 +1,5 @@
 """What the 8-bit paged cache does with calls that were planned and not
-finished: open blocks that have made way."""
+finished: open blocks that have made way, rows that were never appended."""
 import numpy as np
 import pytest
 import torch
@@ -79,3 +79,53 @@ def test_forks_and_copies_leave_lost_blocks_behind(prec, dh, pairs):
             for i in (0, pairs // 2, pairs - 1):
                 x = b.r.held_rows(src[i], side, 1, int(want[i]))
                 assert np.array_equal(got[i, :len(x)], x) and not got[i, len(x):].any()
+
+
+def test_read_gives_what_was_appended():
+    """Neither a planned call's positions before their rows came, nor those of a call that another has taken the place of."""
+    b = history("bf16", 32, [256, 40, 100], n_pages=10, seed=3)
+    b.c.tppsd_cache_truncate(ints([0]))                       # its pages are free, their codes are still there
+    b.r.truncate([0], [0])
+    c, R = b.c, 200
+
+    def reads(layer, s, n):
+        """The rows of s are its first n positions and nothing else."""
+        k, v = (torch.full((1, R, 2, 32), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        c.tppsd_cache_read(layer, None, R, k, v, seqs=ints([s]))
+        for side, got in ((0, values(k)), (1, values(v))):
+            want = b.r.held_rows(s, side, layer, n)
+            assert np.array_equal(got[0, :n], want), (layer, s, side)
+            assert (got[0, n:] == 7.0).all(), (layer, s, side)
+
+    b.begin(130, seqs=[1, 2], counts=[130, 60])
+    for layer in (0, 1):
+        reads(layer, 1, 40)
+        reads(layer, 2, 100)
+    k, v = b.rand(2, 130, 2, 32), b.rand(2, 130, 2, 32)
+    c.tppsd_cache_append(0, k, v)
+    b.r.append(0, values(k), values(v))
+    reads(0, 1, 170)
+    reads(0, 2, 160)
+    reads(1, 1, 40)
+    reads(1, 2, 100)
+    c.tppsd_cache_attend(1, b.rand(2, 130, 2, 32), k, v)
+    b.r.append(1, values(k), values(v))
+    reads(1, 1, 170)
+    assert c.tppsd_cache_status() == 0
+    # the call is dropped: by another call, by a truncation, by a fork
+    c.tppsd_cache_begin(1, ints([0]))
+    reads(0, 2, 64 + 36)                                      # (60 new positions: its block is still in the ring)
+    assert c.tppsd_cache_status() == 0
+    for op in (lambda: c.tppsd_cache_truncate(ints([0])), lambda: c.tppsd_cache_fork(ints([-1]), ints([-1])),
+               lambda: c.tppsd_cache_copy(tp.Cache(2, 2, 2, 32, "bf16", 1, 64), ints([0]), ints([0]))):
+        b.begin(20, seqs=[2])
+        for layer in (0, 1):
+            c.tppsd_cache_append(layer, k[:1, :20].contiguous(), v[:1, :20].contiguous())
+            b.r.append(layer, values(k[:1, :20]), values(v[:1, :20]))
+            reads(layer, 2, 120)
+        op()
+        reads(0, 2, 100)
+    assert c.tppsd_cache_status() == 0
+    # sequence 1's open block made way for the dropped call's last one
+    reads(0, 1, 0)
+    assert c.tppsd_cache_status() == OPEN
