@@ -416,7 +416,9 @@ int tppsd_timing_read(tppsd_state *s, tppsd_timing *out);
 /* n_heads query heads share n_kv_heads key/value heads (a divisor): query head
  * h reads head h / (n_heads / n_kv_heads). d_head 16, 32, 64 or 128; prec: type
  * of q, k, v, o and the tails. n_pages 0: max_seqs ceil(max_events / 64), enough
- * for every sequence at its longest; fewer where sequences share pages. */
+ * for every sequence at its longest; fewer where sequences share pages. Limits:
+ * 2^20 sequences, 2^30 positions of one, 2^26 pages, 2^30 entries of the table
+ * (max_seqs ceil(max_events / 64)). */
 typedef struct {
   int32_t n_layers, n_heads, n_kv_heads, d_head, prec;
   int32_t max_seqs, max_events, n_pages;

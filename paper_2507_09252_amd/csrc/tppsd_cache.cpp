@@ -24,6 +24,8 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 constexpr int MAX_SEQS = 1 << 20, MAX_EVENTS = 1 << 30, MAX_PAGES = 1 << 26;
+// entries of all sequences' tables: a plan sums pages over its rows in 32 bits
+constexpr long long MAX_TABLE = 1LL << 30;
 
 int check_cfg(const tppsd_cache_cfg *c, CacheDev *d) {
   if (!c) return fail(TPPSD_E_ARG, "null cache configuration");
@@ -39,6 +41,8 @@ int check_cfg(const tppsd_cache_cfg *c, CacheDev *d) {
   const long long np = (c->max_events + CACHE_BLOCK - 1LL) / CACHE_BLOCK;
   const long long pages = c->n_pages ? c->n_pages : np * c->max_seqs;
   if (pages < 1 || pages > MAX_PAGES) return fail(TPPSD_E_ARG, "%lld pages outside 1..%d", pages, MAX_PAGES);
+  if (np * c->max_seqs > MAX_TABLE)
+    return fail(TPPSD_E_ARG, "%d sequences of %lld pages: more than %lld table entries", c->max_seqs, np, MAX_TABLE);
   d->L = c->n_layers;
   d->H = c->n_heads;
   d->KV = c->n_kv_heads;
