@@ -26,6 +26,16 @@ constexpr size_t ALIGN = 256;
 constexpr int MAX_SEQS = 1 << 20, MAX_EVENTS = 1 << 30, MAX_PAGES = 1 << 26;
 // entries of all sequences' tables: a plan sums pages over its rows in 32 bits
 constexpr long long MAX_TABLE = 1LL << 30;
+// products of the limits pass 64 bits: sizes are summed in 128, and no workspace has more bytes than this
+typedef unsigned __int128 bytes_t;
+constexpr bytes_t MAX_BYTES = (bytes_t)1 << 48;
+
+struct Entry {
+  const char *name;
+  size_t off;
+};
+constexpr int N_ENTRIES = 6;
+bytes_t view(CacheDev *c, char *ws, Entry *entries);
 
 int check_cfg(const tppsd_cache_cfg *c, CacheDev *d) {
   if (!c) return fail(TPPSD_E_ARG, "null cache configuration");
@@ -52,25 +62,20 @@ int check_cfg(const tppsd_cache_cfg *c, CacheDev *d) {
   d->NP = (int)np;
   d->n_pages = (int)pages;
   d->max_events = c->max_events;
+  if (view(d, nullptr, nullptr) > MAX_BYTES) return fail(TPPSD_E_ARG, "a workspace of more than 2^48 bytes");
   return TPPSD_OK;
 }
 
-struct Entry {
-  const char *name;
-  size_t off;
-};
-constexpr int N_ENTRIES = 6;
-
-size_t view(CacheDev *c, char *ws, Entry *entries) {
-  size_t off = 0;
+bytes_t view(CacheDev *c, char *ws, Entry *entries) {
+  bytes_t off = 0;
   int n = 0;
-  auto take = [&](auto *&p, size_t bytes, const char *name = nullptr) {
+  auto take = [&](auto *&p, bytes_t bytes, const char *name = nullptr) {
     off = (off + ALIGN - 1) / ALIGN * ALIGN;
-    p = ws ? (std::remove_reference_t<decltype(p)>)(ws + off) : nullptr;
-    if (name && entries) entries[n++] = {name, off};
+    p = ws ? (std::remove_reference_t<decltype(p)>)(ws + (size_t)off) : nullptr;
+    if (name && entries) entries[n++] = {name, (size_t)off};
     off += bytes;
   };
-  const size_t L = c->L, S = c->S, KV = c->KV, N = c->n_pages, dh = c->dh, e = c->bf16 ? 2 : 4;
+  const bytes_t L = c->L, S = c->S, KV = c->KV, N = c->n_pages, dh = c->dh, e = c->bf16 ? 2 : 4;
   take(c->pages, L * N * KV * 2 * CACHE_BLOCK * dh, "pages");
   take(c->scales, L * N * KV * 2 * 4, "scales");
   take(c->tails, L * S * KV * 2 * CACHE_RING * dh * e, "tails");
@@ -94,8 +99,8 @@ size_t view(CacheDev *c, char *ws, Entry *entries) {
   take(c->p_start, S * 4);
   take(c->p_count, S * 4);
   c->max_items = cache_max_items(c->S, c->KV);
-  take(c->items, (size_t)c->max_items * sizeof(CacheItem));
-  take(c->part, cache_part_floats(*c) * 4);
+  take(c->items, (bytes_t)c->max_items * sizeof(CacheItem));
+  take(c->part, (bytes_t)cache_part_floats(*c) * 4);
   take(c->joins, CACHE_JOINS * 4);
   take(c->stash, S * KV * 2 * CACHE_BLOCK * dh * e);
   take(c->status, 4);
@@ -144,7 +149,7 @@ CacheRows packed_rows(const tppsd_cache *c, const tppsd_cache_rows *r) {
 }  // namespace
 
 namespace tppsd {
-size_t cache_view(CacheDev *c, char *d_ws) { return view(c, d_ws, nullptr); }
+size_t cache_view(CacheDev *c, char *d_ws) { return (size_t)view(c, d_ws, nullptr); }
 }  // namespace tppsd
 
 extern "C" {
@@ -153,7 +158,7 @@ int tppsd_cache_bytes(const tppsd_cache_cfg *cfg, size_t *bytes) {
   CacheDev d{};
   if (int rc = check_cfg(cfg, &d)) return rc;
   if (!bytes) return fail(TPPSD_E_ARG, "null output pointer");
-  *bytes = view(&d, nullptr, nullptr);
+  *bytes = (size_t)view(&d, nullptr, nullptr);
   return TPPSD_OK;
 }
 
@@ -173,7 +178,7 @@ int tppsd_cache_create(const tppsd_cache_cfg *cfg, void *d_workspace, size_t ws_
   if (int rc = check_cfg(cfg, &d)) return rc;
   if (!d_workspace || !out) return fail(TPPSD_E_ARG, "null workspace or output pointer");
   if ((uintptr_t)d_workspace % ALIGN) return fail(TPPSD_E_WORKSPACE, "workspace must be 256-byte aligned");
-  const size_t need = view(&d, nullptr, nullptr);
+  const size_t need = (size_t)view(&d, nullptr, nullptr);
   if (ws_bytes < need) return fail(TPPSD_E_WORKSPACE, "workspace has %zu bytes, needs %zu", ws_bytes, need);
   tppsd_cache *c = new (std::nothrow) tppsd_cache();
   if (!c) return fail(TPPSD_E_ARG, "no host memory");

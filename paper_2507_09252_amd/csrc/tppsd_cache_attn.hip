@@ -766,9 +766,10 @@ int cache_max_items(int S, int KV) { return S + 3 * (CACHE_SPLIT_WAVES / 4 / KV 
 // groups states; target x heads x groups <= CACHE_SPLIT_WAVES / 4. A state is
 // output, maximum and sum of up to four tiles of 16 query rows, lane by lane.
 size_t cache_part_floats(const CacheDev &c) {
-  const size_t groups = (size_t)call_groups(c, c.max_events);
-  const size_t few = c.KV * groups * ((size_t)c.S + (size_t)c.S * c.NP / CACHE_MIN_PIECE);
-  return std::min<size_t>(6 * CACHE_SPLIT_WAVES / 4, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
+  const size_t most = 6 * CACHE_SPLIT_WAVES / 4;
+  const size_t groups = std::min(most, c.KV * (size_t)call_groups(c, c.max_events));   // (their product with the rows fits)
+  const size_t few = groups * ((size_t)c.S + (size_t)c.S * c.NP / CACHE_MIN_PIECE);
+  return std::min(most, few) * (2 * 4 + 4 * 4 * (c.dh / 16)) * 64;
 }
 
 void launch_cache_attend(const CacheDev &c, const CacheAttend &call, hipStream_t st, hipEvent_t ev0, hipEvent_t ev1) {

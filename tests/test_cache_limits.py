@@ -31,3 +31,23 @@ def refused(lib, **kw):
                                               (1 << 20, (1 << 10) * 64, True)])
 def test_tables_that_a_plan_cannot_sum(lib, seqs, events, fits):
     assert refused(lib, max_seqs=seqs, max_events=min(events, 1 << 30), n_pages=100) is not fits
+
+
+# bytes that pass 64 bits, or come near: 2 x 64 d_head a page, layer and head
+@pytest.mark.parametrize("kw", [dict(n_layers=65534, n_heads=65535, n_kv_heads=65535, d_head=128, n_pages=1 << 26),
+                                dict(n_layers=32768, n_heads=32768, n_kv_heads=32768, d_head=128, n_pages=1 << 20),
+                                dict(n_layers=32768, n_heads=32768, n_kv_heads=32768, d_head=128, n_pages=1,
+                                     max_seqs=1 << 20, max_events=64)],
+                         ids=["pages", "pages-wrap", "tails"])
+def test_workspaces_past_64_bits(lib, kw):
+    assert refused(lib, **kw)
+
+
+def test_states_of_split_rows_fit(lib):
+    """The partial states of split rows are sized without passing 64 bits: 2^15
+    heads and 2^25 groups of query rows are 2^40 states a page."""
+    base = dict(n_layers=1, n_heads=32768, n_kv_heads=32768, d_head=16, prec=1, n_pages=1)
+    n = [ctypes.c_size_t(), ctypes.c_size_t()]
+    for x, events in zip(n, (1 << 20, 1 << 30)):
+        assert lib.tppsd_cache_bytes(ctypes.byref(cfg(**base, max_seqs=8, max_events=events)), ctypes.byref(x)) == 0
+    assert n[1].value >= n[0].value                      # a longer table, the same states
