@@ -488,7 +488,7 @@ int tppsd_cache_append(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
  * the output are accumulated in fp32. A position whose own visible keys or
  * values are not finite gets NaN; positions that do not see them are not
  * touched. o may be q's memory, not k's or v's. Errors: as tppsd_cache_append; TPPSD_E_ARG
- * also for a scale that is not positive and finite, and for more than 65535
+ * also for a scale that is not positive or, times log2(e), not finite, and for more than 65535
  * groups of query rows (beyond 2^18 positions of eight query heads a key/value head of 128). */
 int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, float scale, int sink,
                        hipStream_t stream);

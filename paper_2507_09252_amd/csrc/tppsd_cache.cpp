@@ -235,7 +235,8 @@ int tppsd_cache_attend(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, 
   if (int rc = check_rows(c->d, rows->v, rows->ldv, c->d.KV, "v")) return rc;
   if (int rc = check_rows(c->d, rows->q, rows->ldq, c->d.H, "q")) return rc;
   if (int rc = check_rows(c->d, rows->o, rows->ldo, c->d.H, "o")) return rc;
-  if (!(scale > 0.f) || !std::isfinite(scale)) return fail(TPPSD_E_ARG, "scale must be positive and finite");
+  if (!(scale > 0.f) || !std::isfinite(scale * 1.4426950408889634f))   // (scores go to base 2)
+    return fail(TPPSD_E_ARG, "scale and scale log2(e) must be positive and finite");
   if (cache_groups(c->d, c->P) > 65535)   // (a dimension of the grid)
     return fail(TPPSD_E_ARG, "%d positions of %d heads a key/value head are too many for one call", c->P, c->d.H / c->d.KV);
   CacheAttend a{};

@@ -3,9 +3,10 @@ the host (no GPU needed)."""
 import ctypes
 
 import pytest
+import torch
 
 from paper_2507_09252_amd import tppsd as tp
-from test_cache_host import ARG, cfg
+from test_cache_host import ARG, cfg, make
 
 
 @pytest.fixture(scope="module")
@@ -51,3 +52,17 @@ def test_states_of_split_rows_fit(lib):
     for x, events in zip(n, (1 << 20, 1 << 30)):
         assert lib.tppsd_cache_bytes(ctypes.byref(cfg(**base, max_seqs=8, max_events=events)), ctypes.byref(x)) == 0
     assert n[1].value >= n[0].value                      # a longer table, the same states
+
+
+def test_scale_whose_base_two_form_overflows(lib):
+    """Scores are taken to base 2: scale log2 e has to be a number too."""
+    h = make(lib)
+    if torch.cuda.is_available():
+        pytest.skip("marks a cache over a made-up address as reset")
+    p = ctypes.c_void_p(1 << 20)
+    rows = tp.CacheRowsC(p, p, p, p, 128, 64, 64, 128)
+    assert lib.tppsd_cache_reset(h, None) == 5
+    assert lib.tppsd_cache_begin(h, 1, 1, None, None, None) == 5
+    for scale, code in ((3e38, ARG), (2e38, 5)):
+        assert lib.tppsd_cache_attend(h, 0, ctypes.byref(rows), scale, 0, None) == code
+    lib.tppsd_cache_destroy(h)
