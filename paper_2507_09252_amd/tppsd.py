@@ -338,6 +338,8 @@ class State:
         parent = parent.to(torch.int32).contiguous()
         if parent.numel() != self.B or parent.device != self.ws.device:
             raise TppsdError(1, f"parent must hold {self.B} sequences on {self.ws.device}")
+        if source.ws.device != self.ws.device:
+            raise TppsdError(1, "states lie on different devices")
         self._parent = parent
         _check(lib().tppsd_state_fork(self.handle, source.handle, _ptr(parent), _stream()))
 
