@@ -231,7 +231,9 @@ int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, i
  * sequence whose parent does not exist, is not its own (to == from) or has
  * more events than to's max_events is left as it is (to == from) or empty and
  * finished (TPPSD_STATUS_SEQUENCE). Within a state a copy draws from counters
- * that neither it nor its parent has used, for up to 4095 forks of a run.
+ * that neither it nor its parent has used, for up to 4095 forks of a run. A round
+ * of `to` that was under way is dropped: tppsd_accept needs a tppsd_verify after
+ * the fork.
  * Errors: TPPSD_E_ARG (null, from's history length + n_gen + to's
  * max_gamma + 1 > to's max_events), TPPSD_E_CONFIG (models or TPPSD_FLAG_CACHE8
  * differ), TPPSD_E_ORDER (from has no prefill), TPPSD_E_HIP. */
@@ -280,7 +282,8 @@ int tppsd_verify_noalloc(tppsd_state *s, int gamma, const tppsd_draft_buf *in, c
  * NULL, gives (u_tau, u_k) per draft position [B, max_gamma, 2] in (0, 1);
  * otherwise they come from the Philox counters (sequence, round, l, ACCEPT).
  * Residual and bonus draws always use Philox. Every pointer in `out` must be
- * valid. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
+ * valid. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no prefill, or a tppsd_state_fork
+ * since the last tppsd_verify), TPPSD_E_HIP. */
 int tppsd_accept(tppsd_state *s, int gamma, const tppsd_draft_buf *draft,
                  const tppsd_verify_buf *verify, const float *d_uniforms,
                  const tppsd_accept_buf *out, hipStream_t stream);

@@ -272,6 +272,7 @@ struct tppsd_state {
   int left_max = -1;               // events the slowest sequence still needs, -1: not known here
   bool windowed = false;           // end times given: a sequence may finish at any event
   bool prefilled = false, draft_ok = false, drafted_this_round = false;
+  bool unverified = false;         // sequences came by a fork and no verify pass has run since
   int32_t *host_ndone = nullptr;   // pinned, 2 slots
   hipEvent_t poll_ev[2] = {nullptr, nullptr};
   // measurement (tppsd_timing_enable): two event sets alternated per round
@@ -1061,6 +1062,13 @@ int do_verify(tppsd_state *s, int gamma, const tppsd_draft_buf *in, const tppsd_
   return hip_check("tppsd_verify");
 }
 
+// do_verify, on behalf of the caller: what it verified may be accepted
+int verify_round(tppsd_state *s, int gamma, const tppsd_draft_buf *in, const tppsd_verify_buf *out, hipStream_t st) {
+  const int rc = do_verify(s, gamma, in, out, st);
+  if (rc == TPPSD_OK) s->unverified = false;
+  return rc;
+}
+
 int do_accept(tppsd_state *s, int gamma, const tppsd_draft_buf *dr, const tppsd_verify_buf *vf, const float *u,
               const tppsd_accept_buf *out, hipStream_t st) {
   AcceptArgs a{};
@@ -1568,6 +1576,7 @@ int tppsd_prefill_window(tppsd_state *s, const float *d_t, const int32_t *d_k, i
   s->n_gen = n_gen;
   s->windowed = d_t_end != nullptr;
   s->left_max = s->windowed ? -1 : n_gen;
+  s->unverified = false;
   s->job_ctx = n0 + n_gen / 2;
   build_forms(s, st);
   if (s->cache8) launch_cache_reset(s->c8, st);
@@ -1638,6 +1647,7 @@ int tppsd_state_fork(tppsd_state *to, tppsd_state *from, const int32_t *d_parent
   to->prefilled = true;
   to->draft_ok = from->draft_ok;
   to->drafted_this_round = false;
+  to->unverified = true;
   return hip_check("tppsd_state_fork");
 }
 
@@ -1682,7 +1692,7 @@ int tppsd_verify(tppsd_state *s, int gamma, const tppsd_draft_buf *in, const tpp
   if (int rc = check_round(s, gamma)) return rc;
   if (int rc = check_draft_buf(in)) return rc;
   if (int rc = check_verify_buf(out)) return rc;
-  return do_verify(s, gamma, in, out, st);
+  return verify_round(s, gamma, in, out, st);
 }
 
 int tppsd_verify_noalloc(tppsd_state *s, int gamma, const tppsd_draft_buf *in, const tppsd_verify_buf *out,
@@ -1709,7 +1719,7 @@ int tppsd_verify_noalloc(tppsd_state *s, int gamma, const tppsd_draft_buf *in, c
   s->u = base + L.u;
   s->logits = (float *)(base + L.logits);
   s->attn_part = (float *)(base + L.attn_part);
-  const int rc = do_verify(s, gamma, in, out, st);
+  const int rc = verify_round(s, gamma, in, out, st);
   s->x = x;
   s->a = a;
   s->q = q;
@@ -1728,6 +1738,7 @@ int tppsd_accept(tppsd_state *s, int gamma, const tppsd_draft_buf *dr, const tpp
   if (int rc = check_draft_buf(dr)) return rc;
   if (int rc = check_verify_buf(vf)) return rc;
   if (int rc = check_accept_buf(out)) return rc;
+  if (s->unverified) return fail(TPPSD_E_ORDER, "sequences were forked since the last tppsd_verify");
   int rc = do_accept(s, gamma, dr, vf, d_uniforms, out, st);
   s->left_max = -1;
   if (!s->drafted_this_round) s->draft_ok = false;   // the draft cache missed this round's events
