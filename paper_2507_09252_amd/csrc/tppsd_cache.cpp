@@ -84,7 +84,6 @@ bytes_t view(CacheDev *c, char *ws, Entry *entries) {
   take(c->refs, N * 4, "refs");
   take(c->held, S * 4);
   take(c->low, S * 4);
-  take(c->lost, S * 4);
   take(c->pend, S * 4);
   take(c->planned, S * 4);
   take(c->came, L * S * 4);

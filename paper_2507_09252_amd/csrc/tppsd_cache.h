@@ -46,9 +46,9 @@ struct CacheDev {
   int32_t *refs;      // [n_pages] sequences that hold the page
   int32_t *held;      // [S] pages held (those of uncommitted blocks too)
   int32_t *low;       // [S] first block whose rows the ring holds
-  int32_t *lost;      // [S] the plan's positions follow an open block that is not in the ring any more
   int32_t *pend;      // [S] positions that the plan brings and that are not committed
-  int32_t *planned;   // [S] number of the last plan that brings the sequence any
+  int32_t *planned;   // [S] twice the number of the last plan that brings the sequence any; 1: behind an open
+                      // block that is not in the ring any more (which a commit settles)
   int32_t *came;      // [L][S] number of the last plan whose rows the layer has
   uint32_t *freeb;    // [ceil(n_pages / 32)] bit set: page is free
   int32_t *owner;     // [S] scratch: which row of a call names the sequence

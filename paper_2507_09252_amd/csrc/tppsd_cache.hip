@@ -135,7 +135,7 @@ __global__ void k_cache_reset(CacheDev c) {
   const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x, n = (size_t)gridDim.x * blockDim.x;
   for (size_t j = i; j < (size_t)c.S * c.NP; j += n) c.table[j] = -1;
   for (size_t j = i; j < (size_t)c.S; j += n)
-    c.lens[j] = c.held[j] = c.low[j] = c.lost[j] = c.pend[j] = c.planned[j] = 0;
+    c.lens[j] = c.held[j] = c.low[j] = c.pend[j] = c.planned[j] = 0;
   for (size_t j = i; j < (size_t)c.L * c.S; j += n) c.came[j] = 0;
   for (size_t j = i; j < (size_t)c.n_pages; j += n) c.refs[j] = 0;
   for (size_t j = i; j < (size_t)(c.n_pages + 31) / 32; j += n) {
@@ -151,8 +151,9 @@ __global__ void k_cache_reset(CacheDev c) {
   }
 }
 
+__device__ __forceinline__ int next_plan(int plan) { return (plan + 1) & 0x3FFFFFFF; }   // (stored doubled as well)
 // a plan in progress is dropped: what it brought is nobody's
-__device__ __forceinline__ void drop_plan(const CacheDev &c) { c.counts[PLAN_ID] += 1; }
+__device__ __forceinline__ void drop_plan(const CacheDev &c) { c.counts[PLAN_ID] = next_plan(c.counts[PLAN_ID]); }
 
 // Plans a call: which sequence each row of the batch names, its first new
 // position and how many it brings; pages for the blocks that become whole; and
@@ -202,7 +203,7 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
   }
   auto top_of = [&](const Row &r) { return r.cnt > 0 ? (r.start + r.cnt - 1) / CACHE_BLOCK : 0; };
   auto need_of = [&](const Row &r) { return r.cnt > 0 ? max(0, (r.start + r.cnt) / CACHE_BLOCK - r.held) : 0; };
-  const int hint = c.counts[2], plan = c.counts[PLAN_ID] + 1;
+  const int hint = c.counts[2], plan = next_plan(c.counts[PLAN_ID]);
   Sums mine = {0, 0, 0}, before;
   each(true, [&](int i, Row &r) {
     const int s = b.seqs ? b.seqs[i] : i;
@@ -254,8 +255,7 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
         const int low = c.low[r.seq];
         const bool lost = open_lost(r.start, low);
         if (lost) atomicOr(c.status, TPPSD_STATUS_OPEN);
-        c.lost[r.seq] = lost;
-        c.planned[r.seq] = plan;
+        c.planned[r.seq] = plan << 1 | (lost ? 1 : 0);
         c.low[r.seq] = max(top_of(r) - 1, lost ? low : min(low, r.start / CACHE_BLOCK));
       }
     }
@@ -308,13 +308,15 @@ __global__ void k_cache_commit(CacheDev c, int B, const int32_t *accept) {
   const int s = c.p_seq[i], cnt = c.p_count[i];
   if (s < 0 || cnt <= 0) return;
   int n = c.p_start[i] + (accept ? min(max(accept[i], 0), cnt) : cnt);
-  if (c.lost[s]) n = c.p_start[i];   // (rows behind a lost block are no good either)
+  const int planned = c.planned[s];
+  if (planned & 1) n = c.p_start[i];   // (rows behind a lost block are no good either)
   if (open_lost(n, c.low[s])) {
     atomicOr(c.status, TPPSD_STATUS_OPEN);
     n = n / CACHE_BLOCK * CACHE_BLOCK;
   }
   c.lens[s] = n;
-  c.pend[s] = c.lost[s] = 0;
+  c.pend[s] = 0;
+  c.planned[s] = planned & ~1;
 }
 
 __global__ void k_cache_truncate(CacheDev c, const int32_t *seqs, const int32_t *lens) {
@@ -671,7 +673,8 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheDev c, int layer, const
   const int len = c.lens[s], pend = c.pend[s], plan = c.counts[PLAN_ID];
   const bool has = c.came[(size_t)layer * c.S + s] == plan;
   int end = has ? len + pend : len;
-  if (!has && (c.planned[s] == plan ? c.lost[s] != 0 : open_lost(len, c.low[s]))) {
+  const int planned = c.planned[s];
+  if (!has && (planned >> 1 == plan ? (planned & 1) != 0 : open_lost(len, c.low[s]))) {
     if (tid == 0) atomicOr(c.status, TPPSD_STATUS_OPEN);
     end = len / CACHE_BLOCK * CACHE_BLOCK;
   }

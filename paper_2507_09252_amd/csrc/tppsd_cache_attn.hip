@@ -94,6 +94,8 @@ template <typename ACT, int DH, typename TO> __device__ __forceinline__ void loa
   }
 }
 
+// bits 15 and 31: the halves of w that are not finite bf16 (an exponent of ones carries into the sign's place)
+__device__ __forceinline__ uint32_t bf_odd(uint32_t w) { return (w & 0x7FFF7FFFu) + 0x00800080u; }
 // halves of w that are not finite bf16, as 0xFFFF
 __device__ __forceinline__ uint32_t bf_bad(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
@@ -104,10 +106,23 @@ __device__ __forceinline__ uint32_t bf_bad(uint32_t w) {
 // as good as masked. (fp32 keys have it from their parts: inf - inf.)
 __device__ __forceinline__ Eight<bf16_t> nan_keys(Eight<bf16_t> k) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) k.w[0][i] |= bf_bad(k.w[0][i]) & 0x00400040u;
+  for (int i = 0; i < 4; ++i) k.w[0][i] |= bf_odd(k.w[0][i]) >> 9 & 0x00400040u;
   return k;
 }
 __device__ __forceinline__ Eight<float> nan_keys(const Eight<float> &k) { return k; }
+// whether any of 8 elements is not finite
+__device__ __forceinline__ bool any_odd(const Eight<bf16_t> &v) {
+  uint32_t x = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x |= bf_odd(v.w[0][i]);
+  return (x & 0x80008000u) != 0u;
+}
+__device__ __forceinline__ bool any_odd(const Eight<float> &v) {
+  bool x = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x |= not_finite(v.at(e));
+  return x;
+}
 
 // The operand of 8 values of a column, four at p and four at p + 16, in parts;
 // clean: those that are not finite as 0, or (bad) 1 in their place and 0 elsewhere.
@@ -376,6 +391,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
 
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, rr = lane & 15, g = lane >> 4;
   const int h = blockIdx.y, G = c.H / c.KV, item = blockIdx.x;
+  const int plan = ONE ? c.counts[PLAN_ID] : 0;
   CacheItem it;
   if (a.whole) {   // rows are not split: the plan's rows say it all
     it.row = item;
@@ -502,11 +518,11 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
         vv.load(vp);
       }
       nan_keys(kk).store(&win.k[row][j]);
+      bad |= in && any_odd(vv);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const ACT v = in ? vv.at(e) : (ACT)0, k = kk.at(e);
         win.v[j + e][row] = v;
-        bad |= not_finite(ld(&v, 0));
         if (ONE && n >= CACHE_BLOCK && row < CACHE_BLOCK) top_up(top_k, ld(&k, 0)), top_up(top_v, ld(&v, 0));
       }
       if (ONE && in && pos >= start) {
@@ -515,7 +531,7 @@ __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void 
         vv.store(to + CACHE_RING * DH);
       }
     }
-    if (ONE && h == 0 && tid == 0) c.came[(size_t)a.layer * c.S + seq] = c.counts[PLAN_ID];
+    if (ONE && h == 0 && tid == 0) c.came[(size_t)a.layer * c.S + seq] = plan;
     any_bad = __syncthreads_or(bad);
     if constexpr (ONE) {
       if (n >= CACHE_BLOCK) {   // the first block is whole: its page
