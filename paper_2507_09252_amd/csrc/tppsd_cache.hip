@@ -123,8 +123,8 @@ __device__ __forceinline__ bool open_lost(int n, int low) { return n % CACHE_BLO
 // Positions of a sequence that another can take over: without the open block
 // where that is lost.
 __device__ __forceinline__ int sound_len(const CacheDev &c, int s) {
-  const int n = c.lens[s];
-  return open_lost(n, c.low[s]) ? n / CACHE_BLOCK * CACHE_BLOCK : n;
+  const int n = c.lens[s], low = c.low[s];
+  return open_lost(n, low) ? n / CACHE_BLOCK * CACHE_BLOCK : n;
 }
 
 // whole pages that a sequence of n positions has to share or copy: never more than it holds
@@ -451,11 +451,12 @@ __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int
   const int i = blockIdx.x;
   if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) drop_plan(c);
   if (!pair_goes(c, c, n, src, dst, i, true)) return;
-  const int s = src[i], d = dst[i], len = sound_len(c, s), np = pages_of(c, s, len);
-  if (blockIdx.y > 0) {
-    copy_tail(c, c, blockIdx.y - 1, gridDim.y - 1, s, d, len);
+  const int s = src[i], d = dst[i];
+  if (blockIdx.y > 0) {   // (the slots of a lost block go along, for nothing: the destination ends before them)
+    copy_tail(c, c, blockIdx.y - 1, gridDim.y - 1, s, d, c.lens[s]);
     return;
   }
+  const int len = sound_len(c, s), np = pages_of(c, s, len);
   pages_drop(c, d, 0, c.held[d]);
   __syncthreads();
   for (int j = threadIdx.x; j < np; j += blockDim.x) {
@@ -524,10 +525,11 @@ __global__ __launch_bounds__(256) void k_copy_data(CacheDev to, CacheDev from, i
   if ((int)blockIdx.x < seq_wgs) {
     const int i = blockIdx.x % n, y = (int)blockIdx.x / n;
     if (!to.p_seq[i]) return;
-    const int s = src[i], d = dst[i], len = sound_len(from, s), np = pages_of(from, s, len);
-    if (y > 0) {
-      copy_tail(to, from, y - 1, Y - 1, s, d, len);
+    const int s = src[i], d = dst[i];
+    if (y > 0) {   // (as in k_cache_fork)
+      copy_tail(to, from, y - 1, Y - 1, s, d, from.lens[s]);
     } else {
+      const int len = sound_len(from, s), np = pages_of(from, s, len);
       for (int j = threadIdx.x; j < np; j += blockDim.x) {
         const int page = from.map[from.table[(size_t)s * from.NP + j]];
         to.table[(size_t)d * to.NP + j] = page;
