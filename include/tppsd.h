@@ -397,7 +397,8 @@ int tppsd_timing_read(tppsd_state *s, tppsd_timing *out);
  * as e4m3 codes with one power-of-two scale for each page, layer, key/value
  * head and side (keys, values): half the bytes of bf16. Codes are
  * rne(x 2^-e), e the least integer >= -100 with max |x| <= 448 2^e over the
- * page's finite elements; elements that are not finite become NaN. A block
+ * page's finite elements; elements that are not finite become NaN (and finite ones
+ * of 31 2^123, 3.3e38, and more may become infinite: keep rows below 2^127). A block
  * that is not full yet is kept as its rows came (in the cache's precision), so
  * an element is rounded once, under the maximum of its whole block.
  *
@@ -468,7 +469,8 @@ int tppsd_cache_reset(tppsd_cache *c, hipStream_t stream);
  * it and the rows before it need are not there (TPPSD_STATUS_PAGES). Pages of
  * positions that do not stay are the sequence's until it gets there or is truncated.
  *
- * A plan that was not committed is dropped. If it appended more than 64
+ * A plan that was not committed is dropped (by the next one, or by a truncation,
+ * fork or copy into this cache). If it appended more than 64
  * positions, the rows of a sequence's open block may have made way for the last
  * ones. Such a block is lost: every call of the sequence sets TPPSD_STATUS_OPEN,
  * its positions see in the block's place what its slots hold now, and its commit
@@ -481,8 +483,9 @@ int tppsd_cache_reset(tppsd_cache *c, hipStream_t stream);
 int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, const int32_t *d_counts,
                       hipStream_t stream);
 
-/* Appends the planned rows of one layer. Every layer is appended once before
- * tppsd_cache_commit. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no plan), TPPSD_E_HIP. */
+/* Appends the planned rows of one layer. Every layer is appended once, here or by
+ * tppsd_cache_attend, before tppsd_cache_commit; again, with the same rows, only
+ * in calls of at most 64 positions. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no plan), TPPSD_E_HIP. */
 int tppsd_cache_append(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, hipStream_t stream);
 
 /* Appends the planned rows of one layer and attends: o = softmax(scale q K^T) V
@@ -513,7 +516,8 @@ int tppsd_cache_truncate(tppsd_cache *c, int n, const int32_t *d_seqs, const int
 
 /* d_dst[j] becomes a copy of sequence d_src[j], j < n <= max_seqs: what it held is freed,
  * whole pages are shared (they are never written again) and the open block's
- * rows copied (TPPSD_STATUS_OPEN: not those of a lost block). A source may be named many times; a pair whose destination
+ * rows copied (TPPSD_STATUS_OPEN: not those of a lost block, or of one whose place
+ * a call in progress of more than 64 positions takes). A source may be named many times; a pair whose destination
  * another pair names before it or as a source is left out
  * (TPPSD_STATUS_SEQUENCE); a pair of two negative numbers is none. Errors: TPPSD_E_ARG, TPPSD_E_ORDER, TPPSD_E_HIP. */
 int tppsd_cache_fork(tppsd_cache *c, int n, const int32_t *d_src, const int32_t *d_dst, hipStream_t stream);

@@ -160,7 +160,9 @@ __device__ __forceinline__ void drop_plan(const CacheDev &c) { c.counts[PLAN_ID]
 // the attention's work items. One workgroup, as many threads as rows (PER rows
 // a thread past 1024, held in registers; 0: any number, in memory): the batch's
 // bookkeeping is a few integers a row, and two sums over the rows are all that
-// threads exchange. 64 rows 2.6 us, 4096 rows 9 us.
+// threads exchange. Plans that take next to no pages: 64 rows 2.9 us, 4096 rows
+// 13 us. Pages are given out by each row's thread one after another, some 0.35 us
+// each: one row of 500 pages 183 us, 48 rows of 40 17, 48 of 500 180, 4096 of one 63.
 template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(CacheDev c, CacheBegin b) {
   __shared__ Sums sums[PLAN_NT / 64];
   const int tid = threadIdx.x, nt = blockDim.x;
@@ -267,8 +269,10 @@ template <int PER> __global__ __launch_bounds__(PLAN_NT) void k_cache_begin(Cach
   if (avail < all.a && b.split_target > 0) all = block_sums(mine, &before, sums);   // (rows were left out)
   // Work items. Rows of about equal length that fill the chip are taken whole.
   // Otherwise pages are dealt out in pieces of a workgroup's share, or, where
-  // many rows leave many remainders, of a third of it. Pieces of a row have
-  // adjoining slots for their partial states.
+  // many rows leave many remainders, of a third of it (ragged rows of 8 heads of
+  // 64, a share and a third: 4 rows of up to 32000 14.2 and 19.4 us, 16 19.6 and
+  // 21.0, 64 of up to 16000 31.8 and 30.2). Pieces of a row have adjoining slots
+  // for their partial states.
   if (b.split_target <= 0) return;   // (the attention reads the rows)
   int chunk = INT32_MAX;
   const int share = (all.b + b.split_target - 1) / b.split_target, parts = b.B * 4 <= b.split_target ? 1 : 3;
@@ -370,7 +374,9 @@ __device__ bool pair_stands(const CacheDev &to, const CacheDev &from, int n, con
 }
 // The same for long lists, once for all pairs, into to.p_seq: the first pair of
 // each destination and the sources are marked in LDS, or for more sequences
-// than that holds in memory.
+// than that holds in memory. Lists of 256 pairs and fewer are looked through by
+// the working kernel (forks in four layers, so and with this launch in front:
+// 256 pairs 11.7 and 10.9 + 2.1 us, 512 20.5 and 19.1 + 3.9, 2048 98 and 87 + 5).
 constexpr int FEW_PAIRS = 256, LDS_SEQS = 12288;
 template <bool LDS>
 __global__ __launch_bounds__(PLAN_NT) void k_cache_pairs(CacheDev to, CacheDev from, int n, const int32_t *src,
@@ -446,7 +452,7 @@ __device__ void copy_tail(const CacheDev &to, const CacheDev &from, int l0, int 
 
 // Grid (pairs, 1 + groups of layers): the table and counters, then the layers'
 // open rows. Latency for few pairs (7: 4 us), memory for many (1792 x 6 layers,
-// 142 MB: 35 us).
+// 142 MB: 36 us).
 __global__ __launch_bounds__(256) void k_cache_fork(CacheDev c, int n, const int32_t *src, const int32_t *dst) {
   const int i = blockIdx.x;
   if (i == 0 && blockIdx.y == 0 && threadIdx.x == 0) drop_plan(c);

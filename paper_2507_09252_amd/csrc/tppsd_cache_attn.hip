@@ -360,9 +360,13 @@ constexpr int min_waves(int dh, int mt, bool bf16) { return !bf16 ? (dh == 128 ?
 //
 // Bound by memory for long rows (32 x 4600 positions, 8 heads of 64, 17 new: 32
 // us a layer, 4.8 TB/s; 32 x 16000 89 us, 5.9 TB/s), by one chain of dependent
-// loads and steps for short ones (5 us for one sequence of 220, 8 for 64 of 550),
-// by the softmax's instructions for chunks (16 rows of up to 1001 new positions
-// after up to 2000: 70 us, 280 TFLOP/s).
+// loads and steps for short ones (fp32, heads of 16: 5 us for one sequence of
+// 220, 10 for 64 of 550). Chunks (16 rows of up to 1001 new positions after up to
+// 2000: 73 us, 270 TFLOP/s) use nothing up: SIMDs issue VALU instructions in 34 %
+// of the launch's cycles and MFMA is busy in 13 %, waves wait 42 % of theirs, and
+// compute units have work in two thirds of them. A wave has about three pages,
+// and around them come the queries' load, the window's staging, one wave's step
+// on the own block while three wait, and the fold.
 template <typename ACT, int DH, int MT, int NW, bool ONE, bool HINT>
 __global__ __launch_bounds__(64 * NW, min_waves(DH, MT, sizeof(ACT) == 2)) void k_cache_attend(CacheDev c, CacheAttend a) {
   typedef Rows<ACT, DH, MT> R;
@@ -747,8 +751,11 @@ int call_groups(const CacheDev &c, int P) {
 }
 
 // Waves of a workgroup: eight where their registers and LDS leave room and
-// either sequences may be long or there are too few workgroups for the chip
-// anyway; four otherwise.
+// either sequences may be long or there are no more workgroups than compute
+// units; four otherwise. Eight and four, bf16 heads of 64, workgroups x positions:
+// 64 x 500 7.9 and 8.6 us, 256 x 500 9.9 and 10.2, 512 x 500 13.2 and 16.7, 2048 x
+// 500 42 and 34, 256 x 1500 14.8 and 16.6, 512 x 4000 42.6 and 49.8, 2048 x 4000
+// equal (186).
 constexpr bool eight_fit(int dh, bool bf16, int mt, bool one) { return one && dh <= (bf16 ? 64 : 32) && mt < 4; }
 int waves_of(const CacheDev &c, int B, int P) {
   const bool one = one_group(c, P);
