@@ -485,7 +485,7 @@ int tppsd_cache_begin(tppsd_cache *c, int B, int n_new, const int32_t *d_seqs, c
 
 /* Appends the planned rows of one layer. Every layer is appended once, here or by
  * tppsd_cache_attend, before tppsd_cache_commit; again, with the same rows, only
- * in calls of at most 64 positions. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no plan), TPPSD_E_HIP. */
+ * in calls of at most 64 positions or from a block's border on. Errors: TPPSD_E_ARG, TPPSD_E_ORDER (no plan), TPPSD_E_HIP. */
 int tppsd_cache_append(tppsd_cache *c, int layer, const tppsd_cache_rows *rows, hipStream_t stream);
 
 /* Appends the planned rows of one layer and attends: o = softmax(scale q K^T) V
